@@ -248,6 +248,83 @@ int polydl_bnorm_fwd(int N, int K, int P, int Q, const float *x, const float *ga
                      void *stream);
 int polydl_activation(int64_t count, float *y, int act, void *stream);
 
+/* ---- layer of experts ---------------------------------------------------------------------------
+ * A mixture of experts: E pairs of weight matrices, of which every token uses k.  The router chooses them and sorts the
+ * T*k (token, choice) pairs, the slots, by expert; the products then take every group of rows through its own matrix; the
+ * weighted sum brings a token's k results together.  All three have their gradients, so that a training step is
+ *   route -> grouped_gemm (rows = tokens) -> grouped_gemm -> combine, and back
+ *   combine_bwd -> grouped_gemm_dx / _dw -> grouped_gemm_dx / _dw (rows = tokens) -> combine (no weights) and route_bwd,
+ * and with few tokens the products can read 4-bit weights (polydl_w4_gemm_bf16).
+ * The plan stays in device memory: no entry point here waits for the device or needs to know the groups' sizes.  None keeps memory
+ * of its own (route takes a workspace), and all may be captured.  Results do not depend on the run: sums have a fixed order.
+ * bfloat16 values are uint16_t bit patterns, products of them exact, sums float32, each result rounded once to nearest even.
+ * Row strides (ld...) count elements and may exceed the row.  Any size, alignment to an element and stride is served; the products are fast
+ * where K, N and the strides are multiples of 8 and the tensors 16-byte aligned.  A pointer to a tensor without
+ * elements may be NULL.  Errors: POLYDL_ERR_BAD_DIMENSION for a size or stride out of range, POLYDL_ERR_UNSUPPORTED for an
+ * activation, type, alignment or size that no kernel serves.
+ *
+ * Values in device memory that are no plan cannot be refused: offsets outside [0, M] are taken as the nearest bound and
+ * an end before its start as an empty group; a row index outside [0, x_rows) stands for a row of zeros, a slot outside [0, M)
+ * for none, an id outside [0, E) for no choice.  Nothing outside the tensors is read or written. */
+typedef enum polydl_type { POLYDL_F32 = 0, POLYDL_BF16 = 1 } polydl_type;
+
+/* Router.  logits [T][E] float32.  ids[t][j]: the expert with the j-th largest logit, the lowest index first among equal ones.  A
+ * logit of -infinity is masked and never chosen: where fewer than k are left, the remaining ids are -1 with weight 0 (a row
+ * of padding has k of them).  NaN counts as larger than every number and makes its row's weights NaN.
+ * weights[t][j] = exp(l_id) / sum_e exp(l_e) over all experts, or with renorm != 0 over the chosen ones.
+ * The plan: slot s of the M = T*k belongs to the expert e with offsets[e] <= s < offsets[e+1], ordered by token inside it;
+ * tokens[s] is its token (-1 from offsets[E] on), slots[t][j] the slot of the pair (-1 where there is none).
+ * offsets has E+1 entries.  workspace: polydl_route_workspace_bytes(T, E) bytes (0 up to 64 tokens; 4-byte aligned, contents undefined
+ * afterwards).  1 <= k <= E, E <= 1024, k <= 32, T*k < 2^31.  T = 0 gives offsets of zeros.
+ * polydl_route_bwd: dlogits [T][E] from dweights [T][k].  p = softmax(logits[t]), g_e = dweights of the choice of e, else 0:
+ * dlogits_e = p_e * (g_e - sum_i p_i g_i); with renorm the weights stand in p's place and logits may be NULL; without,
+ * weights may be. */
+size_t polydl_route_workspace_bytes(int T, int E);
+int polydl_route(int T, int E, int k, const float *logits, int renorm, int32_t *ids, float *weights, int32_t *offsets, int32_t *tokens,
+                 int32_t *slots, void *workspace, size_t workspace_bytes, void *stream);
+int polydl_route_bwd(int T, int E, int k, const float *logits, const int32_t *ids, const float *weights, const float *dweights, int renorm,
+                     float *dlogits, void *stream);
+
+/* Weighted sum: out[t] = sum_j weights[t][j] * y[slots[t][j]], y [M][D] bfloat16, out [T][D] of out_type (polydl_type);
+ * weights NULL: 1 each (the gradient of reading tokens through the plan).  D <= 2^24.
+ * polydl_combine_bwd_bf16: dy[slots[t][j]] = weights[t][j] * dout[t] (bfloat16; rows of y that are no pair's slot are not written),
+ * dweights[t][j] = sum_d dout[t][d] * y[slots[t][j]][d] (float32, 0 without a slot).  dweights may be NULL, then y may be. */
+int polydl_combine_bf16(int T, int k, int M, int D, const uint16_t *y, const int32_t *slots, const float *weights, void *out, int out_type,
+                        void *stream);
+int polydl_combine_bwd_bf16(int T, int k, int M, int D, const uint16_t *dout, const uint16_t *y, const int32_t *slots, const float *weights,
+                            uint16_t *dy, float *dweights, void *stream);
+
+/* Products grouped by expert.  Group e holds the rows offsets[e] .. offsets[e+1]-1 of M (offsets[0] = 0), weights w [E][N][K].
+ *   polydl_grouped_gemm_bf16:    y[s][n] = act(sum_k x[r(s)][k] * w[e][n][k]), r(s) = rows[s], or s with rows NULL (then x_rows = M).
+ *       Rows of y from offsets[E] on are written as zeros.
+ *   polydl_grouped_gemm_dx_bf16: dx[s][k] = act'(h[s][k]) * sum_n dy[s][n] * w[e][n][k]; h [M][K] is what the activation gave
+ *       (act' = 1 where 0 < h, for ReLU6 also h < 6; else 0), not read with POLYDL_ACT_NONE.  Rows from offsets[E] on: zeros.
+ *   polydl_grouped_gemm_dw_bf16: dw[e][n][k] = sum_s dy[s][n] * x[r(s)][k] over the group's rows, zeros for an empty group;
+ *       accumulate != 0 (float32 only) adds to what dw holds.
+ * Results of out_type (polydl_type). */
+int polydl_grouped_gemm_bf16(int E, int M, int N, int K, const int32_t *offsets, const int32_t *rows, int x_rows, const uint16_t *x, int64_t ldx,
+                             const uint16_t *w, void *y, int64_t ldy, int out_type, int act /* polydl_act */, void *stream);
+int polydl_grouped_gemm_dx_bf16(int E, int M, int N, int K, const int32_t *offsets, const uint16_t *dy, int64_t lddy, const uint16_t *w,
+                                const uint16_t *h, int64_t ldh, int act /* polydl_act */, void *dx, int64_t lddx, int out_type, void *stream);
+int polydl_grouped_gemm_dw_bf16(int E, int M, int N, int K, const int32_t *offsets, const uint16_t *dy, int64_t lddy, const int32_t *rows,
+                                int x_rows, const uint16_t *x, int64_t ldx, void *dw, int out_type, int accumulate, void *stream);
+
+/* Products with 4-bit weights, for few rows: y[s][n] = act(sum_g scale[n][g] * sum_{k in g} (q[n][k] - zero[n][g]) * x[r(s)][k]),
+ * groups g of `group` (32, 64 or 128) inputs; grouping by expert and rows as above, offsets NULL with E = 1: all rows.
+ * Right for any number of rows; the weights are read once for every 64 rows of a group.  The codes enter the matrix cores as 16 + q and the 16
+ * leaves again in float32: a row that holds an infinity or NaN, or whose sums of 31 |x| overflow, gives NaN or infinities.
+ * The layout, KT = ceil(K/128) steps and NT = ceil(N/16) tiles:
+ *   q      [E][NT][KT][64][16] bytes, 16-byte aligned: lane l of step s holds row 16*tile + l%16; nibble p (0 = low bits) of its i-th
+ *          32-bit word is the code of input 128*s + 32*i + 8*(l/16) + 2*(p%4) + p/4;
+ *   scales [E][NT][KT*128/group][16] bfloat16, 8-byte aligned;   zeros the same shape, uint8 0 .. 15, or NULL: 8.
+ * Rows past N and inputs past K may hold any code; scales there must be finite.
+ * polydl_w4_pack_bf16 writes it from w [E][N][K]: without zeros scale = max|w|/7 and codes 1 .. 15, with zeros scale =
+ * (max(w,0) - min(w,0))/15; scales rounded to bfloat16 before the codes are found, codes rounded to nearest. */
+int polydl_w4_pack_bf16(int E, int N, int K, int group, const uint16_t *w, uint8_t *q, uint16_t *scales, uint8_t *zeros, void *stream);
+int polydl_w4_gemm_bf16(int E, int M, int N, int K, int group, const int32_t *offsets, const int32_t *rows, int x_rows, const uint16_t *x,
+                        int64_t ldx, const uint8_t *q, const uint16_t *scales, const uint8_t *zeros, void *y, int64_t ldy, int out_type,
+                        int act /* polydl_act */, void *stream);
+
 /* ---- the reuse model (sections "Working set size computation" and "Poly-ranking algorithm") ------
  * polydl_reuse_analyse (declared below, before polydl_reuse_bucket): the working sets of a small loop nest.
  * polydl_reuse_bucket: algorithm "Compute working set sizes w.r.t cache sizes": the n working set

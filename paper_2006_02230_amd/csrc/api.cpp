@@ -50,10 +50,10 @@ static int launch_failed(hipError_t e)
     g_last_hip_error = (int)e;
     return POLYDL_ERR_LAUNCH;
 }
-static int launched(hipError_t e) { return e == hipSuccess ? POLYDL_OK : launch_failed(e); }
+int launched(hipError_t e) { return e == hipSuccess ? POLYDL_OK : launch_failed(e); }
 
 // The kernels are gfx950 code: any other current device (or none) is refused.  Asked once per device.
-static bool on_gfx950()
+bool on_gfx950()
 {
     static std::mutex mu;
     static std::map<int, bool> known;

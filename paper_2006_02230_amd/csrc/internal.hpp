@@ -138,6 +138,10 @@ constexpr size_t kStaticPartialBytes = 64 * 1024 * 1024;
 hipError_t static_scratch_arena(ScratchArena *arena);
 int compute_units();   // of the current device
 
+// api.cpp: whether the kernels run on the current device; the status of a launch
+bool on_gfx950();
+int launched(hipError_t e);
+
 // Workgroups of one launch are all resident at once or run in rounds; either way a compute unit
 // takes a whole number of them, so `tiles % cus` leftover tiles make one more round that most
 // compute units sit out.  When those leftovers would occupy at most half of the compute units,
