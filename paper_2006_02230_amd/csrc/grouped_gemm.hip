@@ -1,13 +1,14 @@
 // Matrix products grouped by expert, bfloat16 operands, float32 sums: the forward product of the rows of each group with
 // the group's weights, and the gradients of the rows and of the weights.
 //
-// One kernel in three forms.  A workgroup owns a tile BM x BN of one group's result and walks the reduction in stages of 64,
-// two stage buffers in LDS; a wave keeps a tile WM x WN in registers as 16x16 results of v_mfma_f32_16x16x32_bf16.
+// One kernel in three forms.  A workgroup owns a tile BM x BN of one group's result and walks the reduction in stages of 32,
+// four stage buffers in LDS; a wave keeps a tile WM x WN in registers as 16x16 results of v_mfma_f32_16x16x32_bf16.
 // An operand lies in LDS as it lies in memory, in units of eight values (16 bytes):
-//   * reduction innermost (both operands of the forward product, the rows of the gradient of the rows): [row][64]; a lane
-//     reads the eight values of its row that one instruction takes.  The unit c of a row is stored in place c ^ (row & 7), so
-//     that the lanes of one read fall on different banks.
-//   * reduction outermost (weights in the gradient of the rows, both operands in that of the weights): [64][columns]; the
+//   * reduction innermost (both operands of the forward product, the rows of the gradient of the rows): [row][32]; a lane
+//     reads the eight values of its row that one instruction takes.  The unit c of a row is stored in place
+//     c ^ (-(row / 4) & 3): the 16 lanes that a wide read serves at a time (0-3, 12-15, 20-23, 24-27 and their like) then fall on
+//     different banks, as they do not with c ^ (row / 4 & 3) (twice the cycles).
+//   * reduction outermost (weights in the gradient of the rows, both operands in that of the weights): [32][columns]; the
 //     transposing LDS read gives a lane four values of its column from four rows.  Blocks of 16 columns are stored in the
 //     block's place ^ a number of the row that differs for the eight rows that half a wave reads at a time.
 // Loads go from memory into LDS without registers; the permutation is applied to the address a lane loads from.  Lanes past an
@@ -26,10 +27,12 @@ namespace polydl {
 typedef __bf16 gg_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float gg_f32x4 __attribute__((ext_vector_type(4)));
 typedef short gg_i16x4 __attribute__((ext_vector_type(4)));
-typedef __attribute__((address_space(3))) void *gg_lds_t;
+typedef int gg_i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t gg_u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kStage = 64;                          // reduction of a stage
+constexpr int kStage = 32;                          // reduction of a stage: of one matrix instruction
+constexpr int kBuffers = 4;                         // stages in LDS
+constexpr int kIndices = 4096;                      // row indices of the reduction kept in LDS at a time
 constexpr uint32_t kFarOffset = 0xfffffff0u;        // out of range of every descriptor here
 constexpr uint64_t kFarRecords = 0xffffffe0ull;     // so that no sum of an offset in range and a load's width reaches 2^32
 
@@ -47,17 +50,32 @@ struct GroupedArgs {
     int row_tiles, col_tiles;      // of one C_e (GROUPED_DW); columns (others)
 };
 
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t gg_rsrc(const char *base, int64_t bytes)
+// A raw buffer descriptor of `bytes` bytes from base (none if negative).
+__device__ __forceinline__ gg_i32x4 gg_rsrc(const char *base, int64_t bytes)
 {
-    const uint64_t n = bytes < 0 ? 0 : (uint64_t)bytes > kFarRecords ? kFarRecords : (uint64_t)bytes;
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<char *>(base), (short)0, (int)(uint32_t)n, 0x00020000);
+    const uint64_t n = bytes < 0 ? 0 : (uint64_t)bytes > kFarRecords ? kFarRecords : (uint64_t)bytes, at = (uint64_t)base;
+    return gg_i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffffu), (int)(uint32_t)n, 0x00020000};
 }
-__device__ __forceinline__ void gg_dma(__amdgpu_buffer_rsrc_t r, void *lds, uint32_t off)
+// Sixteen bytes a lane into LDS at `lds` + 16 * lane; not waited for.  As assembly, because the compiler puts a wait for every such
+// load before each transposing LDS read, whichever buffer it reads (dX 1050 -> 902, dW 820 -> 512 TFLOP/s at 16384 x 4096 x
+// 2048).  Nothing is written to a register; the waits are gg_wait()'s.  The wait states are those that a descriptor or m0 just written needs; nothing else
+// in these kernels uses m0.
+__device__ __forceinline__ void gg_dma(gg_i32x4 rsrc, uint32_t lds, uint32_t off)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (gg_lds_t)lds, 16, (int)off, 0, 0, 0);
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory");
 #else
-    (void)r; (void)lds; (void)off;
+    (void)rsrc; (void)lds; (void)off;
+#endif
+}
+// where a pointer into the workgroup's LDS points
+__device__ __forceinline__ uint32_t gg_lds_offset(const char *lds)
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)lds;
+#else
+    (void)lds;
+    return 0;
 #endif
 }
 __device__ __forceinline__ gg_u32x2 gg_read_tr(const char *lds)
@@ -91,34 +109,32 @@ struct Operand {
     static_assert((kAll % THREADS == 0 || kAll < THREADS) && THREADS % kRow == 0 && kAll % 64 == 0, "whole units, whole waves");
     static_assert(!RED_OUTER || R == 64 || R % 128 == 0, "the block permutation");
 
+    static constexpr bool kIndexed = GATHER && RED_OUTER;        // the reduction's rows are read by index
     const char *base;                 // of the tile; GATHER: of the tensor (RED_OUTER: of the tile's columns in it)
     int64_t ld, bytes;                // from row to row; from base to the end of what may be read
     int red, count;                   // length of the reduction; rows or columns of the tile that exist
     const int32_t *rows;              // GATHER: of the tile's rows (innermost), of the reduction's (outermost)
     int src_rows;
+    const int *index;                 // kIndexed: in LDS, entry k % kIndices is row k's, -1: none
     uint32_t off[DMA ? kUnits : 1];
-    int32_t next[DMA && GATHER && RED_OUTER ? kUnits : 1];       // rows of the next stage
+    int32_t src[kIndexed ? kUnits : 1];                          // rows of the stage to be fetched
     const char *at[!DMA && !RED_OUTER ? kUnits : 1];             // of the unit's row, NULL: none
     lanes_u32x4 held[DMA ? 1 : kUnits];
+    gg_i32x4 rsrc;                    // of the stage to be fetched
 
-    // the permutation: of the blocks of 16 columns in reduction row kr
+    // the permutation: of the blocks of 16 columns in reduction row kr, of the units of row r
     static __device__ __forceinline__ int spread(int kr)
     {
         return R == 64 ? ((kr >> 1) & 1) | ((kr >> 3) & 1) << 1 : (kr & 3) | ((kr >> 3) & 1) << 2;
     }
+    static __device__ __forceinline__ int turn(int r) { return -(r >> 2) & 3; }
     static __device__ __forceinline__ bool mine(int tid) { return kAll >= THREADS || tid < kAll; }
     static __device__ __forceinline__ int lds_row(int tid, int i) { return tid / kRow + i * (THREADS / kRow); }
     // which unit of its row the thread's unit i holds
     static __device__ __forceinline__ int unit_of(int tid, int i)
     {
         const int r = lds_row(tid, i), u = tid % kRow;
-        return RED_OUTER ? u ^ (spread(r) << 1) : u ^ (r & 7);
-    }
-    __device__ __forceinline__ int row_index(int r) const
-    {
-        if (!GATHER) return r;
-        const int s = rows[r];
-        return (unsigned)s < (unsigned)src_rows ? s : -1;
+        return RED_OUTER ? u ^ (spread(r) << 1) : u ^ turn(r);
     }
 
     __device__ __forceinline__ void init(int tid)
@@ -127,49 +143,64 @@ struct Operand {
         for (int i = 0; i < kUnits; ++i) {
             const int r = lds_row(tid, i), u = unit_of(tid, i);
             if constexpr (!RED_OUTER) {
-                const int src = r < count ? row_index(r) : -1;
-                if constexpr (DMA) off[i] = src < 0 ? kFarOffset : (uint32_t)src * (uint32_t)ld + (uint32_t)u * 16u;
-                else at[i] = src < 0 ? nullptr : base + src * ld;
+                int from = r < count ? r : -1;
+                if (GATHER && from >= 0) {
+                    from = rows[r];
+                    if ((unsigned)from >= (unsigned)src_rows) from = -1;
+                }
+                if constexpr (DMA) off[i] = from < 0 ? kFarOffset : (uint32_t)from * (uint32_t)ld + (uint32_t)u * 16u;
+                else at[i] = from < 0 ? nullptr : base + from * ld;
             } else if constexpr (DMA) {
                 off[i] = u * 8 < count ? (GATHER ? 0u : (uint32_t)r * (uint32_t)ld) + (uint32_t)u * 16u : kFarOffset;
-                if constexpr (GATHER) next[i] = r < red ? row_index(r) : -1;
             }
         }
     }
+    // kIndexed: the indices of rows k0 .. k0 + kIndices - 1 of the reduction into LDS
+    __device__ __forceinline__ void load_indices(int *to, int k0, int tid) const
+    {
+        for (int i = tid; i < kIndices && k0 + i < red; i += THREADS) {
+            const int r = rows[k0 + i];
+            to[i] = (unsigned)r < (unsigned)src_rows ? r : -1;
+        }
+    }
 
-    // Stage s: asked for into `lds` (DMA), or into registers.
-    __device__ __forceinline__ void fetch(int s, char *lds, int tid)
+    // A stage is fetched in three steps: begin() once, unit() for each unit, commit() when registers held it.
+    __device__ __forceinline__ void begin(int s, int tid)
+    {
+        const int k0 = s * kStage;
+        if constexpr (DMA) {
+            const int64_t skip = RED_OUTER ? (GATHER ? 0 : (int64_t)k0 * ld) : (int64_t)k0 * 2;
+            rsrc = gg_rsrc(base + skip, bytes - skip);
+        }
+        if constexpr (kIndexed) {
+#pragma unroll
+            for (int i = 0; i < kUnits; ++i) {
+                const int k = k0 + lds_row(tid, i);
+                src[i] = k < red ? index[k % kIndices] : -1;
+            }
+        }
+    }
+    __device__ __forceinline__ void unit(int s, int i, char *lds, int tid)
     {
         if (!mine(tid)) return;
         const int k0 = s * kStage;
         if constexpr (DMA) {
             const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-            const int64_t skip = RED_OUTER ? (GATHER ? 0 : (int64_t)k0 * ld) : (int64_t)k0 * 2;
-            const __amdgpu_buffer_rsrc_t r = gg_rsrc(base + skip, bytes - skip);
-#pragma unroll
-            for (int i = 0; i < kUnits; ++i) {
-                uint32_t o = off[i];
-                if constexpr (!RED_OUTER) {
-                    if (k0 + unit_of(tid, i) * 8 >= red) o = kFarOffset;
-                } else if constexpr (GATHER) {
-                    o = next[i] < 0 || o == kFarOffset ? kFarOffset : (uint32_t)next[i] * (uint32_t)ld + o;
-                    const int k = k0 + kStage + lds_row(tid, i);
-                    next[i] = k < red ? row_index(k) : -1;
-                }
-                gg_dma(r, lds + (i * THREADS + wave * 64) * 16, o);
+            uint32_t o = off[i];
+            if constexpr (!RED_OUTER) {
+                if (k0 + unit_of(tid, i) * 8 >= red) o = kFarOffset;
+            } else if constexpr (GATHER) {
+                o = src[i] < 0 || o == kFarOffset ? kFarOffset : (uint32_t)src[i] * (uint32_t)ld + o;
             }
+            gg_dma(rsrc, gg_lds_offset(lds) + (uint32_t)(i * THREADS + wave * 64) * 16u, o);
         } else {
-#pragma unroll
-            for (int i = 0; i < kUnits; ++i) {
-                held[i] = lanes_u32x4{0u, 0u, 0u, 0u};
-                const int u = unit_of(tid, i) * 8;
-                if constexpr (!RED_OUTER) {
-                    if (at[i] && k0 + u < red) held[i] = load_unit8(reinterpret_cast<const uint16_t *>(at[i]) + k0 + u, red - k0 - u);
-                } else {
-                    const int k = k0 + lds_row(tid, i);
-                    const int src = k < red && u < count ? row_index(k) : -1;
-                    if (src >= 0) held[i] = load_unit8(reinterpret_cast<const uint16_t *>(base + src * ld) + u, count - u);
-                }
+            held[i] = lanes_u32x4{0u, 0u, 0u, 0u};
+            const int u = unit_of(tid, i) * 8;
+            if constexpr (!RED_OUTER) {
+                if (at[i] && k0 + u < red) held[i] = load_unit8(reinterpret_cast<const uint16_t *>(at[i]) + k0 + u, red - k0 - u);
+            } else {
+                const int k = k0 + lds_row(tid, i), from = k < red && u < count ? (kIndexed ? src[i] : k) : -1;
+                if (from >= 0) held[i] = load_unit8(reinterpret_cast<const uint16_t *>(base + from * ld) + u, count - u);
             }
         }
     }
@@ -182,14 +213,14 @@ struct Operand {
         }
     }
 
-    // What one instruction takes of rows r0 .. r0+15, values kk*32 .. kk*32+31 of the stage.
-    static __device__ __forceinline__ lanes_u32x4 operand(const char *lds, int r0, int kk, int lane)
+    // What one instruction takes of rows r0 .. r0+15.
+    static __device__ __forceinline__ lanes_u32x4 operand(const char *lds, int r0, int lane)
     {
         if constexpr (!RED_OUTER) {
             const int r = r0 + (lane & 15);
-            return *reinterpret_cast<const lanes_u32x4 *>(lds + r * (kStage * 2) + (((kk * 4 + (lane >> 4)) ^ (lane & 7)) * 16));
+            return *reinterpret_cast<const lanes_u32x4 *>(lds + r * (kStage * 2) + (((lane >> 4) ^ turn(lane & 15)) * 16));
         } else {
-            const int kr = kk * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
+            const int kr = (lane >> 4) * 8 + ((lane & 15) >> 2);
             const char *at = lds + kr * (R * 2) + ((r0 >> 4) ^ spread(kr)) * 32 + (lane & 3) * 8;
             const gg_u32x2 lo = gg_read_tr(at), hi = gg_read_tr(at + 4 * R * 2);   // spread(kr + 4) == spread(kr) here
             return lanes_u32x4{lo[0], lo[1], hi[0], hi[1]};
@@ -197,12 +228,23 @@ struct Operand {
     }
 };
 
+// s_waitcnt of the gfx9 encoding: vmcnt N (bits 3:0, 15:14), lgkmcnt 0 (11:8), expcnt left alone
+template <int N>
+__device__ __forceinline__ void gg_wait()
+{
+#if defined(__HIP_DEVICE_COMPILE__)
+    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | 0x70);
+#endif
+}
+
 template <int FORM, int BM, int BN, int WM, int WN, bool DMA, bool GATHER, bool OUT_F32>
 struct GroupedTile {
     static constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
     using A = Operand<BM, kThreads, FORM == GROUPED_DW, DMA, GATHER && FORM == GROUPED_FWD>;
     using B = Operand<BN, kThreads, FORM != GROUPED_FWD, DMA, GATHER && FORM == GROUPED_DW>;
-    static constexpr int kStageBytes = A::kBytes + B::kBytes, kLds = 2 * kStageBytes;
+    static constexpr int kStageBytes = A::kBytes + B::kBytes, kIndexBytes = B::kIndexed ? kIndices * 4 : 0;
+    static constexpr int kLds = kBuffers * kStageBytes + kIndexBytes;
+    static constexpr bool kDma = DMA;
 };
 
 template <class T, int FORM, int BM, int BN, int WM, int WN, bool OUT_F32>
@@ -242,8 +284,11 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         c0 = (int64_t)m0 * p.ldc + n0;
         h0 = (int64_t)m0 * p.ldh + n0;
     } else {
-        const int per = p.row_tiles * p.col_tiles, id = die_order((int)blockIdx.x, (int)gridDim.x), e = id / per;
-        const int m = (id - e * per) / p.col_tiles, n = id - e * per - m * p.col_tiles;
+        // groups differ in length, so every die takes an eighth of each one's tiles, another eighth from group to group
+        const int per = p.row_tiles * p.col_tiles, eighth = (per + 7) >> 3, at = (int)blockIdx.x >> 3, e = at / eighth;
+        const int id = (((int)blockIdx.x + e) & 7) * eighth + at - e * eighth;
+        if (id >= per) return;
+        const int m = id / p.col_tiles, n = id - m * p.col_tiles;
         const GroupRows g = group_rows(p.offsets, e, p.E, p.M);
         rows = min(BM, p.out_rows - m * BM);
         cols = min(BN, p.cols - n * BN);
@@ -272,41 +317,90 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
 #pragma unroll
         for (int j = 0; j < NI; ++j) acc[i][j] = gg_f32x4{0.f, 0.f, 0.f, 0.f};
 
+    // In step s the matrix cores work on stage s, which is in registers, while stage s+1 is read from LDS and stage s+4 is asked for,
+    // a load between the products of two rows of results, into the buffer that stage s has left.  DMA: three stages are under way
+    // at any time; s+1 is waited for when the loads behind it are all that is left.
     if (stages > 0) {
-        A.init(tid);
-        B.init(tid);
-        A.fetch(0, grouped_lds, tid);
-        B.fetch(0, grouped_lds + T::A::kBytes, tid);
-        A.commit(grouped_lds, tid);
-        B.commit(grouped_lds + T::A::kBytes, tid);
-        wait_vmcnt0();
-        __syncthreads();
-        for (int s = 0; s < stages; ++s) {
-            char *now = grouped_lds + (s & 1) * T::kStageBytes, *then = grouped_lds + ((s & 1) ^ 1) * T::kStageBytes;
-            if (s + 1 < stages) {
-                A.fetch(s + 1, then, tid);
-                B.fetch(s + 1, then + T::A::kBytes, tid);
+        constexpr int kAhead = T::kDma ? kBuffers : 2, kLoads = T::A::kUnits + T::B::kUnits;
+        int *const index = reinterpret_cast<int *>(grouped_lds + kBuffers * T::kStageBytes);
+        const auto buffer = [&](int s) { return grouped_lds + s % kBuffers * T::kStageBytes; };
+        const auto load = [&](int s, int i) {
+            if (i < T::A::kUnits) A.unit(s, i, buffer(s), tid);
+            else B.unit(s, i - T::A::kUnits, buffer(s) + T::A::kBytes, tid);
+        };
+        const auto fetch = [&](int s) {
+            A.begin(s, tid);
+            B.begin(s, tid);
+#pragma unroll
+            for (int i = 0; i < kLoads; ++i) load(s, i);
+        };
+        const auto commit = [&](int s) {
+            A.commit(buffer(s), tid);
+            B.commit(buffer(s) + T::A::kBytes, tid);
+        };
+        // the n-th operand of a stage: the columns', then the rows'
+        const auto read = [&](int s, int n, lanes_u32x4 (&a)[MI], lanes_u32x4 (&b)[NI]) {
+            if (n < NI) b[n] = T::B::operand(buffer(s) + T::A::kBytes, wn + n * 16, lane);
+            else a[n - NI] = T::A::operand(buffer(s), wm + (n - NI) * 16, lane);
+        };
+        const auto step = [&](int s, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI], lanes_u32x4 (&b_next)[NI]) {
+            commit(s + 1);
+            // this wave's part of stage s+1 has landed, and it has what it read of stage s
+            if (T::kDma && T::A::mine(tid) && T::B::mine(tid)) gg_wait<(kBuffers - 2) * kLoads>();
+            else if (T::kDma && T::B::mine(tid)) gg_wait<(kBuffers - 2) * T::B::kUnits>();
+            else gg_wait<0>();
+            __builtin_amdgcn_s_barrier();
+            __builtin_amdgcn_sched_barrier(0);
+            if (T::B::kIndexed && (s + kAhead) % (kIndices / kStage) == 0) {     // the next indices, rarely
+                B.load_indices(index, (s + kAhead) * kStage, tid);
+                __syncthreads();
             }
+            // the reads of the next stage and the loads of a later one between the products: issued in one go, they hold
+            // the matrix cores up while the LDS takes them in
+            constexpr int kReads = MI + NI, kSpread = MI > 2 ? MI - 1 : MI;
 #pragma unroll
-            for (int kk = 0; kk < kStage / 32; ++kk) {
-                lanes_u32x4 a[MI], b[NI];
-#pragma unroll
-                for (int j = 0; j < NI; ++j) b[j] = T::B::operand(now + T::A::kBytes, wn + j * 16, kk, lane);
-#pragma unroll
-                for (int i = 0; i < MI; ++i) a[i] = T::A::operand(now, wm + i * 16, kk, lane);
+            for (int i = 0; i < MI; ++i) {
                 // columns as the instruction's rows: a lane then holds four neighbouring columns of one row of the result
 #pragma unroll
-                for (int i = 0; i < MI; ++i)
+                for (int j = 0; j < NI; ++j) acc[i][j] = gg_mfma(b[j], a[i], acc[i][j]);
+                if (i == 0) {
+                    A.begin(s + kAhead, tid);
+                    B.begin(s + kAhead, tid);
+                }
 #pragma unroll
-                    for (int j = 0; j < NI; ++j) acc[i][j] = gg_mfma(b[j], a[i], acc[i][j]);
+                for (int n = i * kReads / kSpread; n < (i + 1) * kReads / kSpread && n < kReads; ++n) read(s + 1, n, a_next, b_next);
+#pragma unroll
+                for (int l = i * kLoads / MI; l < (i + 1) * kLoads / MI; ++l) load(s + kAhead, l);
+                __builtin_amdgcn_sched_barrier(0);
             }
-            if (s + 1 < stages) {
-                A.commit(then, tid);
-                B.commit(then + T::A::kBytes, tid);
-            }
-            wait_vmcnt0();
+        };
+        lanes_u32x4 a0[MI], b0[NI], a1[MI], b1[NI];
+        A.init(tid);
+        B.init(tid);
+        if constexpr (T::B::kIndexed) {
+            B.index = index;
+            B.load_indices(index, 0, tid);
             __syncthreads();
         }
+        if constexpr (T::kDma) {
+#pragma unroll
+            for (int s = 0; s < kBuffers; ++s) fetch(s);   // stages past the last read as zeros, without memory
+            gg_wait<0>();
+        } else {
+            fetch(0);
+            commit(0);
+            fetch(1);
+        }
+        __syncthreads();
+#pragma unroll
+        for (int n = 0; n < MI + NI; ++n) read(0, n, a0, b0);
+        for (int s = 0; s < stages; s += 2) {
+            step(s, a0, b0, a1, b1);
+            if (s + 1 >= stages) break;
+            step(s + 1, a1, b1, a0, b0);
+        }
+        gg_wait<0>();                                      // no load into LDS outlives the workgroup's use of it
+        __syncthreads();
     }
 
     const bool whole = (p.ldc & 3) == 0 && ((uintptr_t)p.c & 15) == 0;       // four results at a time
@@ -389,7 +483,7 @@ static hipError_t grouped_run(const GroupedProblem &q, hipStream_t st)
     int64_t tiles;
     if (FORM == GROUPED_DW) {
         a.row_tiles = (q.out_rows + BM - 1) / BM;
-        tiles = (int64_t)q.E * a.row_tiles * a.col_tiles;
+        tiles = ((int64_t)a.row_tiles * a.col_tiles + 7) / 8 * 8 * q.E;
     } else {
         // each group, and the slots behind the last, may end in a partial tile
         const int64_t groups = q.M < q.E + 1 ? q.M : q.E + 1;
