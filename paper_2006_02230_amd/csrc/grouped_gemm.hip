@@ -237,6 +237,9 @@ __device__ __forceinline__ void gg_wait()
 #endif
 }
 
+// four floats at any of their addresses
+struct __attribute__((packed, aligned(4))) Floats4 { gg_f32x4 v; };
+
 template <int FORM, int BM, int BN, int WM, int WN, bool DMA, bool GATHER, bool OUT_F32>
 struct GroupedTile {
     static constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
@@ -403,55 +406,66 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         __syncthreads();
     }
 
-    const bool whole = (p.ldc & 3) == 0 && ((uintptr_t)p.c & 15) == 0;       // four results at a time
+    // Out through LDS, each wave through a part of its own: a lane then stores 16 bytes and the lanes of a row follow one another.
+    // Straight from the registers rows went out in pieces of 32 bytes, and the activation's results came in two at a time
+    // (dX of 16384 x 4096 x 2048 with ReLU: 476 us).
+    constexpr int kUnit = OUT_F32 ? 4 : 8, kAcrossUnits = WN / kUnit;                   // values and units of a row
+    constexpr int kRoom = kBuffers * T::kStageBytes / (T::kThreads / 64) / (kAcrossUnits * 16), kRows = kRoom < WM ? kRoom : WM;
+    static_assert(kRows % 16 == 0 && WM % kRows == 0 && (kAcrossUnits & 7) == 0 && 64 % kAcrossUnits == 0, "whole tiles and rows");
+    char *const mine = grouped_lds + wave * (kRows * kAcrossUnits * 16);
 #pragma unroll
-    for (int i = 0; i < MI; ++i) {
-        const int r = wm + i * 16 + (lane & 15);
-        if (r >= rows) continue;
+    for (int r0 = 0; r0 < WM; r0 += kRows) {
 #pragma unroll
-        for (int j = 0; j < NI; ++j) {
-            const int n = wn + j * 16 + (lane >> 4) * 4, left = cols - n;
-            if (left <= 0) continue;
-            gg_f32x4 v = acc[i][j];
-            if constexpr (FORM == GROUPED_FWD) {
+        for (int i = 0; i < kRows / 16; ++i)
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    // comparisons that let NaN through, as the formula does
-                    if (p.act != POLYDL_ACT_NONE) v[q] = v[q] < 0.f ? 0.f : v[q];
-                    if (p.act == POLYDL_ACT_RELU6) v[q] = v[q] > 6.f ? 6.f : v[q];
-                }
-            }
-            if constexpr (FORM == GROUPED_DX) {
-                if (p.act != POLYDL_ACT_NONE) {
-                    const uint16_t *h = p.h + h0 + (int64_t)r * p.ldh + n;
+            for (int j = 0; j < NI; ++j) {
+                gg_f32x4 v = acc[r0 / 16 + i][j];
+                if constexpr (FORM == GROUPED_FWD) {
 #pragma unroll
                     for (int q = 0; q < 4; ++q) {
-                        const float x = q < left ? bf16_lo(h[q]) : 0.f;
-                        const bool open = x > 0.f && (p.act == POLYDL_ACT_RELU || x < 6.f);
-                        v[q] = open ? v[q] : 0.f;
+                        // comparisons that let NaN through, as the formula does
+                        if (p.act != POLYDL_ACT_NONE) v[q] = v[q] < 0.f ? 0.f : v[q];
+                        if (p.act == POLYDL_ACT_RELU6) v[q] = v[q] > 6.f ? 6.f : v[q];
+                    }
+                }
+                const int r = i * 16 + (lane & 15), n = j * 16 + (lane >> 4) * 4;
+                char *at = mine + (r * kAcrossUnits + ((n / kUnit) ^ (r & 7))) * 16;
+                if constexpr (OUT_F32) *reinterpret_cast<gg_f32x4 *>(at) = v;
+                else *reinterpret_cast<gg_u32x2 *>(at + (n & 4) * 2) = gg_u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+            }
+#pragma unroll
+        for (int i = 0; i < kRows * kAcrossUnits / 64; ++i) {
+            const int r = i * (64 / kAcrossUnits) + lane / kAcrossUnits, u = lane % kAcrossUnits;
+            const int row = wm + r0 + r, n = wn + u * kUnit, left = cols - n;
+            lanes_u32x4 v = *reinterpret_cast<const lanes_u32x4 *>(mine + (r * kAcrossUnits + (u ^ (r & 7))) * 16);
+            if (row >= rows || left <= 0) continue;
+            const int64_t at = c0 + (int64_t)row * p.ldc + n;
+            if constexpr (FORM == GROUPED_DX) {
+                if (p.act != POLYDL_ACT_NONE) {
+                    const uint16_t *h = p.h + h0 + (int64_t)row * p.ldh + n;
+                    const lanes_u32x4 x = kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit)) : load_unit4(h);
+#pragma unroll
+                    for (int q = 0; q < kUnit; ++q) {
+                        const float y = q & 1 ? bf16_hi(x[q >> 1]) : bf16_lo(x[q >> 1]);
+                        const bool open = y > 0.f && (p.act == POLYDL_ACT_RELU || y < 6.f);
+                        if constexpr (OUT_F32) v[q] = open ? v[q] : 0u;
+                        else v[q >> 1] &= open ? 0xffffffffu : q & 1 ? 0x0000ffffu : 0xffff0000u;
                     }
                 }
             }
-            const int64_t at = c0 + (int64_t)r * p.ldc + n;
             if constexpr (OUT_F32) {
                 float *c = static_cast<float *>(p.c) + at;
-                if (whole && left >= 4) {
-                    if (p.accumulate) v += *reinterpret_cast<gg_f32x4 *>(c);
-                    *reinterpret_cast<gg_f32x4 *>(c) = v;
+                gg_f32x4 f = __builtin_bit_cast(gg_f32x4, v);
+                if (left >= 4) {
+                    if (p.accumulate) f += reinterpret_cast<const Floats4 *>(c)->v;
+                    reinterpret_cast<Floats4 *>(c)->v = f;
                 } else {
 #pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (q < left) c[q] = p.accumulate ? c[q] + v[q] : v[q];
+                    for (int q = 0; q < 3; ++q)
+                        if (q < left) c[q] = p.accumulate ? c[q] + f[q] : f[q];
                 }
             } else {
-                uint16_t *c = static_cast<uint16_t *>(p.c) + at;
-                if (whole && left >= 4) {
-                    *reinterpret_cast<gg_u32x2 *>(c) = gg_u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q)
-                        if (q < left) c[q] = bf16_one(v[q]);
-                }
+                store_unit8(static_cast<uint16_t *>(p.c) + at, v, left);
             }
         }
     }

@@ -62,6 +62,13 @@ __device__ __forceinline__ uint16_t bf16_one(float x) { return (uint16_t)bf16_pa
 struct __attribute__((packed, aligned(2))) Unit8 { lanes_u32x4 v; };
 __device__ __forceinline__ lanes_u32x4 load_unit8(const uint16_t *p) { return reinterpret_cast<const Unit8 *>(p)->v; }
 __device__ __forceinline__ void store_unit8(uint16_t *p, lanes_u32x4 v) { reinterpret_cast<Unit8 *>(p)->v = v; }
+// four of them, zeros behind
+struct __attribute__((packed, aligned(2))) Unit4 { uint32_t v[2]; };
+__device__ __forceinline__ lanes_u32x4 load_unit4(const uint16_t *p)
+{
+    const Unit4 u = *reinterpret_cast<const Unit4 *>(p);
+    return lanes_u32x4{u.v[0], u.v[1], 0u, 0u};
+}
 // the first n of them (0 <= n <= 8), zeros for the rest; nothing past them is read
 __device__ __forceinline__ lanes_u32x4 load_unit8(const uint16_t *p, int n)
 {
