@@ -24,41 +24,56 @@ __device__ __forceinline__ int die_order(int id, int total)
     return x * q + min(x, r) + (id >> 3);
 }
 
-// The tile of workgroup `id` among the tiles of `height` rows of all groups times `col_tiles`: false where there is none.
-// Four column tiles at a time, down the rows.
+// The tiles of `height` rows of all groups times `col_tiles`, four column tiles at a time down the rows.  The first 64 groups'
+// counts stay in a wave's registers, the others are read again for every tile.
 struct GroupTile { int e, lo, hi, m, n; };
-__device__ __forceinline__ bool find_tile(const int32_t *offsets, int E, int M, int height, int col_tiles, int id, GroupTile *t)
-{
-    const int lane = threadIdx.x & 63;
-    int total = 0;
-    for (int e0 = 0; e0 <= E; e0 += 64) {
-        const GroupRows g = group_rows(offsets, min(e0 + lane, E), E, M);
-        total += lane_of(wave_prefix(e0 + lane <= E ? (g.hi - g.lo + height - 1) / height : 0), 63);
+struct GroupTiles {
+    const int32_t *offsets;
+    int E, M, height, col_tiles;
+    int total;
+    GroupRows first;               // of group `lane`
+    int first_upto;                // row tiles of the groups up to it
+
+    __device__ __forceinline__ int count(int e, const GroupRows &g) const { return e <= E ? (g.hi - g.lo + height - 1) / height : 0; }
+    __device__ __forceinline__ GroupRows rows(int e) const { return group_rows(offsets, min(e, E), E, M); }
+
+    __device__ __forceinline__ void init(const int32_t *offsets_, int E_, int M_, int height_, int col_tiles_)
+    {
+        offsets = offsets_; E = E_; M = M_; height = height_; col_tiles = col_tiles_;
+        const int lane = threadIdx.x & 63;
+        first = rows(lane);
+        first_upto = wave_prefix(count(lane, first));
+        total = lane_of(first_upto, 63);
+        for (int e0 = 64; e0 <= E; e0 += 64) total += lane_of(wave_prefix(count(e0 + lane, rows(e0 + lane))), 63);
+        total *= col_tiles;
     }
-    total *= col_tiles;
-    if (id >= total) return false;
-    id = die_order(id, total);
-    int before = 0;
-    for (int e0 = 0; e0 <= E; e0 += 64) {
-        const GroupRows g = group_rows(offsets, min(e0 + lane, E), E, M);
-        const int tiles = e0 + lane <= E ? (g.hi - g.lo + height - 1) / height : 0;
-        const int upto = wave_prefix(tiles) * col_tiles;
-        const unsigned long long past = __ballot(id < before + upto);
-        if (past) {
-            const int l = __builtin_ctzll(past), rows = lane_of(tiles, l);
-            const int at = id - before - (lane_of(upto, l) - rows * col_tiles);
-            const int band = at / max(rows * 4, 1), n0 = band * 4, width = max(min(4, col_tiles - n0), 1), in = at - band * rows * 4;
-            t->e = e0 + l;
-            t->lo = lane_of(g.lo, l);
-            t->hi = lane_of(g.hi, l);
-            t->m = in / width;
-            t->n = n0 + in - t->m * width;
-            // offsets that are none (groups that overlap many times) may make the sums above wrap around
-            return (unsigned)t->m < (unsigned)rows && (unsigned)t->n < (unsigned)col_tiles;
+    // the id-th tile; false where there is none
+    __device__ __forceinline__ bool find(int id, GroupTile *t) const
+    {
+        if (id >= total) return false;
+        const int lane = threadIdx.x & 63;
+        id = die_order(id, total);
+        int before = 0;
+        for (int e0 = 0; e0 <= E; e0 += 64) {
+            const GroupRows g = e0 ? rows(e0 + lane) : first;
+            const int tiles = count(e0 + lane, g), upto = (e0 ? wave_prefix(tiles) : first_upto) * col_tiles;
+            const unsigned long long past = __ballot(id < before + upto);
+            if (past) {
+                const int l = __builtin_ctzll(past), high = lane_of(tiles, l);
+                const int at = id - before - (lane_of(upto, l) - high * col_tiles);
+                const int band = at / max(high * 4, 1), n0 = band * 4, width = max(min(4, col_tiles - n0), 1), in = at - band * high * 4;
+                t->e = e0 + l;
+                t->lo = lane_of(g.lo, l);
+                t->hi = lane_of(g.hi, l);
+                t->m = in / width;
+                t->n = n0 + in - t->m * width;
+                // offsets that are none (groups that overlap many times) may make the sums above wrap around
+                return (unsigned)t->m < (unsigned)high && (unsigned)t->n < (unsigned)col_tiles;
+            }
+            before += lane_of(upto, 63);
         }
-        before += lane_of(upto, 63);
+        return false;
     }
-    return false;
-}
+};
 
 }  // namespace polydl

@@ -17,6 +17,7 @@
 // the host.
 #include <hip/hip_runtime.h>
 #include <atomic>
+#include <type_traits>
 #include "experts.hpp"
 #include "gemm_core.hpp"
 #include "group_tiles.hpp"
@@ -246,9 +247,16 @@ struct GroupedTile {
     using A = Operand<BM, kThreads, FORM == GROUPED_DW, DMA, GATHER && FORM == GROUPED_FWD>;
     using B = Operand<BN, kThreads, FORM != GROUPED_FWD, DMA, GATHER && FORM == GROUPED_DW>;
     static constexpr int kStageBytes = A::kBytes + B::kBytes, kIndexBytes = B::kIndexed ? kIndices * 4 : 0;
-    static constexpr int kLds = kBuffers * kStageBytes + kIndexBytes;
     static constexpr bool kDma = DMA;
+    // The workgroups of the forward product and of the gradient of the rows, whose tiles are alike, take tile after tile; those of the gradient of
+    // the weights take one each, as the groups' lengths come, and their results leave through the stages' LDS.
+    static constexpr bool kLoops = FORM != GROUPED_DW;
+    static constexpr int kOutAt = kLoops ? kBuffers * kStageBytes : 0, kOutBytes = kLoops ? kThreads / 64 * 4096 : kBuffers * kStageBytes;
+    static constexpr int kLds = kLoops ? kOutAt + kOutBytes : kBuffers * kStageBytes + kIndexBytes;
 };
+
+// What a finished tile leaves by: its rows and columns that exist, its first result, that of `h`.
+struct GroupedOut { int rows, cols; int64_t c0, h0; };
 
 template <class T, int FORM, int BM, int BN, int WM, int WN, bool OUT_F32>
 __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
@@ -260,124 +268,195 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
 
     typename T::A A;
     typename T::B B;
-    int rows, cols, stages;            // of the tile that exist
-    int64_t c0;                        // its first result
-    int64_t h0 = 0;
-    if constexpr (FORM != GROUPED_DW) {
-        GroupTile t;
-        if (!find_tile(p.offsets, p.E, p.M, BM, p.col_tiles, (int)blockIdx.x, &t)) return;
-        const int m0 = t.lo + t.m * BM, n0 = t.n * BN;
-        rows = min(BM, t.hi - m0);
-        cols = min(BN, p.cols - n0);
-        stages = t.e < p.E ? (p.red + kStage - 1) / kStage : 0;   // slots behind the last group: a result of zeros
-        const int e = min(t.e, p.E - 1);
-        A.rows = p.rows ? p.rows + m0 : nullptr;
-        A.base = FORM == GROUPED_FWD && A.rows ? p.a : p.a + m0 * p.lda;
-        A.bytes = (int64_t)(FORM == GROUPED_FWD && A.rows ? p.src_rows - 1 : rows - 1) * p.lda + (int64_t)p.red * 2;
-        A.red = p.red;
-        A.count = rows;
-        if constexpr (FORM == GROUPED_FWD) {
-            B.base = p.b + ((int64_t)e * p.cols + n0) * p.ldb;
-            B.bytes = (int64_t)(cols - 1) * p.ldb + (int64_t)p.red * 2;
-        } else {
-            B.base = p.b + (int64_t)e * p.red * p.ldb + (int64_t)n0 * 2;
-            B.bytes = (int64_t)(p.red - 1) * p.ldb + (int64_t)cols * 2;
-        }
-        B.red = p.red;
-        c0 = (int64_t)m0 * p.ldc + n0;
-        h0 = (int64_t)m0 * p.ldh + n0;
-    } else {
-        // groups differ in length, so every die takes an eighth of each one's tiles, another eighth from group to group
-        const int per = p.row_tiles * p.col_tiles, eighth = (per + 7) >> 3, at = (int)blockIdx.x >> 3, e = at / eighth;
-        const int id = (((int)blockIdx.x + e) & 7) * eighth + at - e * eighth;
-        if (id >= per) return;
-        const int m = id / p.col_tiles, n = id - m * p.col_tiles;
-        const GroupRows g = group_rows(p.offsets, e, p.E, p.M);
-        rows = min(BM, p.out_rows - m * BM);
-        cols = min(BN, p.cols - n * BN);
-        const int red = g.hi - g.lo;
-        stages = (red + kStage - 1) / kStage;
-        A.rows = nullptr;
-        A.base = p.a + g.lo * p.lda + (int64_t)m * BM * 2;
-        A.bytes = (int64_t)(red - 1) * p.lda + (int64_t)rows * 2;
-        A.red = red;
-        A.count = rows;
-        B.rows = p.rows ? p.rows + g.lo : nullptr;
-        B.base = p.b + (p.rows ? 0 : g.lo * p.ldb) + (int64_t)n * BN * 2;
-        B.bytes = (int64_t)((p.rows ? p.src_rows : red) - 1) * p.ldb + (int64_t)cols * 2;
-        B.red = red;
-        c0 = ((int64_t)e * p.out_rows + (int64_t)m * BM) * p.ldc + (int64_t)n * BN;
-    }
     A.ld = p.lda;
     B.ld = p.ldb;
-    B.count = cols;
     A.src_rows = B.src_rows = p.src_rows;
-    if constexpr (FORM != GROUPED_DW) B.rows = nullptr;
+    A.rows = B.rows = nullptr;
+    GroupTiles tiles;
+    if constexpr (FORM != GROUPED_DW) tiles.init(p.offsets, p.E, p.M, BM, p.col_tiles);
 
-    gg_f32x4 acc[MI][NI];
-#pragma unroll
-    for (int i = 0; i < MI; ++i)
-#pragma unroll
-        for (int j = 0; j < NI; ++j) acc[i][j] = gg_f32x4{0.f, 0.f, 0.f, 0.f};
-
+    // The operands and the result of tile `id`, and its stages; -1: there is no such tile.
+    const auto find = [&](int id, GroupedOut &out) {
+        if constexpr (FORM != GROUPED_DW) {
+            GroupTile t;
+            if (!tiles.find(id, &t)) return -1;
+            const int m0 = t.lo + t.m * BM, n0 = t.n * BN, e = min(t.e, p.E - 1);
+            out.rows = min(BM, t.hi - m0);
+            out.cols = min(BN, p.cols - n0);
+            const bool gathered = FORM == GROUPED_FWD && p.rows;
+            A.rows = gathered ? p.rows + m0 : nullptr;
+            A.base = gathered ? p.a : p.a + m0 * p.lda;
+            A.bytes = (int64_t)(gathered ? p.src_rows - 1 : out.rows - 1) * p.lda + (int64_t)p.red * 2;
+            if constexpr (FORM == GROUPED_FWD) {
+                B.base = p.b + ((int64_t)e * p.cols + n0) * p.ldb;
+                B.bytes = (int64_t)(out.cols - 1) * p.ldb + (int64_t)p.red * 2;
+            } else {
+                B.base = p.b + (int64_t)e * p.red * p.ldb + (int64_t)n0 * 2;
+                B.bytes = (int64_t)(p.red - 1) * p.ldb + (int64_t)out.cols * 2;
+            }
+            A.red = B.red = p.red;
+            out.c0 = (int64_t)m0 * p.ldc + n0;
+            out.h0 = (int64_t)m0 * p.ldh + n0;
+            A.count = out.rows;
+            B.count = out.cols;
+            return t.e < p.E ? (p.red + kStage - 1) / kStage : 0;   // slots behind the last group: a result of zeros
+        } else {
+            // groups differ in length, so every die takes an eighth of each one's tiles, another eighth from group to group
+            const int per = p.row_tiles * p.col_tiles, eighth = (per + 7) >> 3, at = id >> 3, e = at / eighth;
+            const int in = ((id + e) & 7) * eighth + at - e * eighth;
+            if (in >= per) return -1;
+            const int m = in / p.col_tiles, n = in - m * p.col_tiles;
+            const GroupRows g = group_rows(p.offsets, e, p.E, p.M);
+            const int red = g.hi - g.lo;
+            out.rows = min(BM, p.out_rows - m * BM);
+            out.cols = min(BN, p.cols - n * BN);
+            A.base = p.a + g.lo * p.lda + (int64_t)m * BM * 2;
+            A.bytes = (int64_t)(red - 1) * p.lda + (int64_t)out.rows * 2;
+            B.rows = p.rows ? p.rows + g.lo : nullptr;
+            B.base = p.b + (p.rows ? 0 : g.lo * p.ldb) + (int64_t)n * BN * 2;
+            B.bytes = (int64_t)((p.rows ? p.src_rows : red) - 1) * p.ldb + (int64_t)out.cols * 2;
+            A.red = B.red = red;
+            out.c0 = ((int64_t)e * p.out_rows + (int64_t)m * BM) * p.ldc + (int64_t)n * BN;
+            out.h0 = 0;
+            A.count = out.rows;
+            B.count = out.cols;
+            return (red + kStage - 1) / kStage;
+        }
+    };
     // In step s the matrix cores work on stage s, which is in registers, while stage s+1 is read from LDS and stage s+4 is asked for,
     // a load between the products of two rows of results, into the buffer that stage s has left.  DMA: three stages are under way
     // at any time; s+1 is waited for when the loads behind it are all that is left.
-    if (stages > 0) {
-        constexpr int kAhead = T::kDma ? kBuffers : 2, kLoads = T::A::kUnits + T::B::kUnits;
-        int *const index = reinterpret_cast<int *>(grouped_lds + kBuffers * T::kStageBytes);
-        const auto buffer = [&](int s) { return grouped_lds + s % kBuffers * T::kStageBytes; };
-        const auto load = [&](int s, int i) {
-            if (i < T::A::kUnits) A.unit(s, i, buffer(s), tid);
-            else B.unit(s, i - T::A::kUnits, buffer(s) + T::A::kBytes, tid);
-        };
-        const auto fetch = [&](int s) {
-            A.begin(s, tid);
-            B.begin(s, tid);
+    constexpr int kAhead = T::kDma ? kBuffers : 2, kLoads = T::A::kUnits + T::B::kUnits;
+    int *const index = reinterpret_cast<int *>(grouped_lds + kBuffers * T::kStageBytes);
+    const auto buffer = [&](int s) { return grouped_lds + s % kBuffers * T::kStageBytes; };
+    const auto load = [&](int s, int i) {
+        if (i < T::A::kUnits) A.unit(s, i, buffer(s), tid);
+        else B.unit(s, i - T::A::kUnits, buffer(s) + T::A::kBytes, tid);
+    };
+    const auto fetch = [&](int s) {
+        A.begin(s, tid);
+        B.begin(s, tid);
 #pragma unroll
-            for (int i = 0; i < kLoads; ++i) load(s, i);
-        };
-        const auto commit = [&](int s) {
-            A.commit(buffer(s), tid);
-            B.commit(buffer(s) + T::A::kBytes, tid);
-        };
-        // the n-th operand of a stage: the columns', then the rows'
-        const auto read = [&](int s, int n, lanes_u32x4 (&a)[MI], lanes_u32x4 (&b)[NI]) {
-            if (n < NI) b[n] = T::B::operand(buffer(s) + T::A::kBytes, wn + n * 16, lane);
-            else a[n - NI] = T::A::operand(buffer(s), wm + (n - NI) * 16, lane);
-        };
-        const auto step = [&](int s, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI], lanes_u32x4 (&b_next)[NI]) {
-            commit(s + 1);
-            // this wave's part of stage s+1 has landed, and it has what it read of stage s
-            if (T::kDma && T::A::mine(tid) && T::B::mine(tid)) gg_wait<(kBuffers - 2) * kLoads>();
-            else if (T::kDma && T::B::mine(tid)) gg_wait<(kBuffers - 2) * T::B::kUnits>();
-            else gg_wait<0>();
-            __builtin_amdgcn_s_barrier();
-            __builtin_amdgcn_sched_barrier(0);
-            if (T::B::kIndexed && (s + kAhead) % (kIndices / kStage) == 0) {     // the next indices, rarely
-                B.load_indices(index, (s + kAhead) * kStage, tid);
-                __syncthreads();
+        for (int i = 0; i < kLoads; ++i) load(s, i);
+    };
+    const auto commit = [&](int s) {
+        A.commit(buffer(s), tid);
+        B.commit(buffer(s) + T::A::kBytes, tid);
+    };
+    // waits until this wave's loads are down to those of BEHIND stages (or to none), then for the other waves
+    const auto land = [&](auto behind) {
+        constexpr int kBehind = T::kDma ? decltype(behind)::value : 0;
+        if (T::A::mine(tid) && T::B::mine(tid)) gg_wait<kBehind * kLoads>();
+        else if (T::B::mine(tid)) gg_wait<kBehind * T::B::kUnits>();
+        else gg_wait<0>();
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // the n-th operand of a stage: the columns', then the rows'
+    const auto read = [&](int s, int n, lanes_u32x4 (&a)[MI], lanes_u32x4 (&b)[NI]) {
+        if (n < NI) b[n] = T::B::operand(buffer(s) + T::A::kBytes, wn + n * 16, lane);
+        else a[n - NI] = T::A::operand(buffer(s), wm + (n - NI) * 16, lane);
+    };
+    gg_f32x4 acc[MI][NI];
+    const auto step = [&](int s, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI], lanes_u32x4 (&b_next)[NI]) {
+        commit(s + 1);
+        land(std::integral_constant<int, kBuffers - 2>{});        // stage s+1; and this wave has what it read of stage s
+        if (T::B::kIndexed && (s + kAhead) % (kIndices / kStage) == 0) {     // the next indices, rarely
+            B.load_indices(index, (s + kAhead) * kStage, tid);
+            __syncthreads();
+        }
+        // the reads of the next stage and the loads of a later one between the products: issued in one go, they hold
+        // the matrix cores up while the LDS takes them in
+        constexpr int kReads = MI + NI, kSpread = MI > 2 ? MI - 1 : MI;
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            // columns as the instruction's rows: a lane then holds four neighbouring columns of one row of the result
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = gg_mfma(b[j], a[i], acc[i][j]);
+            if (i == 0) {
+                A.begin(s + kAhead, tid);
+                B.begin(s + kAhead, tid);
             }
-            // the reads of the next stage and the loads of a later one between the products: issued in one go, they hold
-            // the matrix cores up while the LDS takes them in
-            constexpr int kReads = MI + NI, kSpread = MI > 2 ? MI - 1 : MI;
 #pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                // columns as the instruction's rows: a lane then holds four neighbouring columns of one row of the result
+            for (int n = i * kReads / kSpread; n < (i + 1) * kReads / kSpread && n < kReads; ++n) read(s + 1, n, a_next, b_next);
 #pragma unroll
-                for (int j = 0; j < NI; ++j) acc[i][j] = gg_mfma(b[j], a[i], acc[i][j]);
-                if (i == 0) {
-                    A.begin(s + kAhead, tid);
-                    B.begin(s + kAhead, tid);
+            for (int l = i * kLoads / MI; l < (i + 1) * kLoads / MI; ++l) load(s + kAhead, l);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+    // Out through LDS, each wave through a part of its own: a lane then stores 16 bytes and the lanes of a row follow one another.
+    // Straight from the registers rows went out in pieces of 32 bytes, and the activation's results came in two at a time
+    // (dX of 16384 x 4096 x 2048 with ReLU: 476 us).
+    constexpr int kUnit = OUT_F32 ? 4 : 8, kAcrossUnits = WN / kUnit;                   // values and units of a row
+    constexpr int kRoom = T::kOutBytes / (T::kThreads / 64) / (kAcrossUnits * 16), kRows = kRoom < WM ? kRoom : WM;
+    static_assert(kRows % 16 == 0 && WM % kRows == 0 && (kAcrossUnits & 7) == 0 && 64 % kAcrossUnits == 0, "whole tiles and rows");
+    char *const mine = grouped_lds + T::kOutAt + wave * (kRows * kAcrossUnits * 16);
+    const auto leave = [&](const GroupedOut &out) {
+        // the compiler may not know that the lane is the same for every tile: it would keep all the addresses below in registers
+        // through the products, and spill
+        int lane = tid & 63;
+        if constexpr (T::kLoops) asm volatile("" : "+v"(lane));
+#pragma unroll
+        for (int r0 = 0; r0 < WM; r0 += kRows) {
+#pragma unroll
+            for (int i = 0; i < kRows / 16; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j) {
+                    gg_f32x4 v = acc[r0 / 16 + i][j];
+                    if constexpr (FORM == GROUPED_FWD) {
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            // comparisons that let NaN through, as the formula does
+                            if (p.act != POLYDL_ACT_NONE) v[q] = v[q] < 0.f ? 0.f : v[q];
+                            if (p.act == POLYDL_ACT_RELU6) v[q] = v[q] > 6.f ? 6.f : v[q];
+                        }
+                    }
+                    const int r = i * 16 + (lane & 15), n = j * 16 + (lane >> 4) * 4;
+                    char *at = mine + (r * kAcrossUnits + ((n / kUnit) ^ (r & 7))) * 16;
+                    if constexpr (OUT_F32) *reinterpret_cast<gg_f32x4 *>(at) = v;
+                    else *reinterpret_cast<gg_u32x2 *>(at + (n & 4) * 2) = gg_u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
                 }
 #pragma unroll
-                for (int n = i * kReads / kSpread; n < (i + 1) * kReads / kSpread && n < kReads; ++n) read(s + 1, n, a_next, b_next);
+            for (int i = 0; i < kRows * kAcrossUnits / 64; ++i) {
+                const int r = i * (64 / kAcrossUnits) + lane / kAcrossUnits, u = lane % kAcrossUnits;
+                const int row = wm + r0 + r, n = wn + u * kUnit, left = out.cols - n;
+                lanes_u32x4 v = *reinterpret_cast<const lanes_u32x4 *>(mine + (r * kAcrossUnits + (u ^ (r & 7))) * 16);
+                if (row >= out.rows || left <= 0) continue;
+                const int64_t at = out.c0 + (int64_t)row * p.ldc + n;
+                if constexpr (FORM == GROUPED_DX) {
+                    if (p.act != POLYDL_ACT_NONE) {
+                        const uint16_t *h = p.h + out.h0 + (int64_t)row * p.ldh + n;
+                        const lanes_u32x4 x = kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit)) : load_unit4(h);
 #pragma unroll
-                for (int l = i * kLoads / MI; l < (i + 1) * kLoads / MI; ++l) load(s + kAhead, l);
-                __builtin_amdgcn_sched_barrier(0);
+                        for (int q = 0; q < kUnit; ++q) {
+                            const float y = q & 1 ? bf16_hi(x[q >> 1]) : bf16_lo(x[q >> 1]);
+                            const bool open = y > 0.f && (p.act == POLYDL_ACT_RELU || y < 6.f);
+                            if constexpr (OUT_F32) v[q] = open ? v[q] : 0u;
+                            else v[q >> 1] &= open ? 0xffffffffu : q & 1 ? 0x0000ffffu : 0xffff0000u;
+                        }
+                    }
+                }
+                if constexpr (OUT_F32) {
+                    float *c = static_cast<float *>(p.c) + at;
+                    gg_f32x4 f = __builtin_bit_cast(gg_f32x4, v);
+                    if (left >= 4) {
+                        if (p.accumulate) f += reinterpret_cast<const Floats4 *>(c)->v;
+                        reinterpret_cast<Floats4 *>(c)->v = f;
+                    } else {
+#pragma unroll
+                        for (int q = 0; q < 3; ++q)
+                            if (q < left) c[q] = p.accumulate ? c[q] + f[q] : f[q];
+                    }
+                } else {
+                    store_unit8(static_cast<uint16_t *>(p.c) + at, v, left);
+                }
             }
-        };
-        lanes_u32x4 a0[MI], b0[NI], a1[MI], b1[NI];
+        }
+    };
+    // asks for the first stages of the tile that find() has set up
+    const auto start = [&]() {
+        int tid = threadIdx.x;
+        if constexpr (T::kLoops) asm volatile("" : "+v"(tid));       // as in leave()
         A.init(tid);
         B.init(tid);
         if constexpr (T::B::kIndexed) {
@@ -388,85 +467,47 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         if constexpr (T::kDma) {
 #pragma unroll
             for (int s = 0; s < kBuffers; ++s) fetch(s);   // stages past the last read as zeros, without memory
-            gg_wait<0>();
         } else {
             fetch(0);
             commit(0);
             fetch(1);
         }
-        __syncthreads();
-#pragma unroll
-        for (int n = 0; n < MI + NI; ++n) read(0, n, a0, b0);
-        for (int s = 0; s < stages; s += 2) {
-            step(s, a0, b0, a1, b1);
-            if (s + 1 >= stages) break;
-            step(s + 1, a1, b1, a0, b0);
-        }
-        gg_wait<0>();                                      // no load into LDS outlives the workgroup's use of it
-        __syncthreads();
-    }
+    };
 
-    // Out through LDS, each wave through a part of its own: a lane then stores 16 bytes and the lanes of a row follow one another.
-    // Straight from the registers rows went out in pieces of 32 bytes, and the activation's results came in two at a time
-    // (dX of 16384 x 4096 x 2048 with ReLU: 476 us).
-    constexpr int kUnit = OUT_F32 ? 4 : 8, kAcrossUnits = WN / kUnit;                   // values and units of a row
-    constexpr int kRoom = kBuffers * T::kStageBytes / (T::kThreads / 64) / (kAcrossUnits * 16), kRows = kRoom < WM ? kRoom : WM;
-    static_assert(kRows % 16 == 0 && WM % kRows == 0 && (kAcrossUnits & 7) == 0 && 64 % kAcrossUnits == 0, "whole tiles and rows");
-    char *const mine = grouped_lds + wave * (kRows * kAcrossUnits * 16);
+    int id = (int)blockIdx.x;
+    GroupedOut now;
+    int stages = find(id, now);
+    if (stages < 0) return;
+    if (stages > 0) start();
+    while (true) {
 #pragma unroll
-    for (int r0 = 0; r0 < WM; r0 += kRows) {
+        for (int i = 0; i < MI; ++i)
 #pragma unroll
-        for (int i = 0; i < kRows / 16; ++i)
+            for (int j = 0; j < NI; ++j) acc[i][j] = gg_f32x4{0.f, 0.f, 0.f, 0.f};
+        if (stages > 0) {
+            lanes_u32x4 a0[MI], b0[NI], a1[MI], b1[NI];
+            land(std::integral_constant<int, kBuffers - 1>{});
 #pragma unroll
-            for (int j = 0; j < NI; ++j) {
-                gg_f32x4 v = acc[r0 / 16 + i][j];
-                if constexpr (FORM == GROUPED_FWD) {
-#pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        // comparisons that let NaN through, as the formula does
-                        if (p.act != POLYDL_ACT_NONE) v[q] = v[q] < 0.f ? 0.f : v[q];
-                        if (p.act == POLYDL_ACT_RELU6) v[q] = v[q] > 6.f ? 6.f : v[q];
-                    }
-                }
-                const int r = i * 16 + (lane & 15), n = j * 16 + (lane >> 4) * 4;
-                char *at = mine + (r * kAcrossUnits + ((n / kUnit) ^ (r & 7))) * 16;
-                if constexpr (OUT_F32) *reinterpret_cast<gg_f32x4 *>(at) = v;
-                else *reinterpret_cast<gg_u32x2 *>(at + (n & 4) * 2) = gg_u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+            for (int n = 0; n < MI + NI; ++n) read(0, n, a0, b0);
+            for (int s = 0; s < stages; s += 2) {
+                step(s, a0, b0, a1, b1);
+                if (s + 1 >= stages) break;
+                step(s + 1, a1, b1, a0, b0);
             }
-#pragma unroll
-        for (int i = 0; i < kRows * kAcrossUnits / 64; ++i) {
-            const int r = i * (64 / kAcrossUnits) + lane / kAcrossUnits, u = lane % kAcrossUnits;
-            const int row = wm + r0 + r, n = wn + u * kUnit, left = cols - n;
-            lanes_u32x4 v = *reinterpret_cast<const lanes_u32x4 *>(mine + (r * kAcrossUnits + (u ^ (r & 7))) * 16);
-            if (row >= rows || left <= 0) continue;
-            const int64_t at = c0 + (int64_t)row * p.ldc + n;
-            if constexpr (FORM == GROUPED_DX) {
-                if (p.act != POLYDL_ACT_NONE) {
-                    const uint16_t *h = p.h + h0 + (int64_t)row * p.ldh + n;
-                    const lanes_u32x4 x = kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit)) : load_unit4(h);
-#pragma unroll
-                    for (int q = 0; q < kUnit; ++q) {
-                        const float y = q & 1 ? bf16_hi(x[q >> 1]) : bf16_lo(x[q >> 1]);
-                        const bool open = y > 0.f && (p.act == POLYDL_ACT_RELU || y < 6.f);
-                        if constexpr (OUT_F32) v[q] = open ? v[q] : 0u;
-                        else v[q >> 1] &= open ? 0xffffffffu : q & 1 ? 0x0000ffffu : 0xffff0000u;
-                    }
-                }
-            }
-            if constexpr (OUT_F32) {
-                float *c = static_cast<float *>(p.c) + at;
-                gg_f32x4 f = __builtin_bit_cast(gg_f32x4, v);
-                if (left >= 4) {
-                    if (p.accumulate) f += reinterpret_cast<const Floats4 *>(c)->v;
-                    reinterpret_cast<Floats4 *>(c)->v = f;
-                } else {
-#pragma unroll
-                    for (int q = 0; q < 3; ++q)
-                        if (q < left) c[q] = p.accumulate ? c[q] + f[q] : f[q];
-                }
-            } else {
-                store_unit8(static_cast<uint16_t *>(p.c) + at, v, left);
-            }
+            land(std::integral_constant<int, 0>{});        // no wave reads the stages any more, no load is under way
+        }
+        if constexpr (!T::kLoops) {
+            leave(now);
+            return;
+        } else {
+            // the next tile's first stages come in while this one's results leave
+            GroupedOut next;
+            id += (int)gridDim.x;
+            stages = find(id, next);
+            if (stages > 0) start();
+            leave(now);
+            if (stages < 0) return;
+            now = next;
         }
     }
 }
@@ -504,6 +545,10 @@ static hipError_t grouped_run(const GroupedProblem &q, hipStream_t st)
         tiles = (q.M + groups * (BM - 1)) / BM * a.col_tiles;
     }
     if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+    if (T::kLoops) {
+        const int64_t fit = (int64_t)compute_units() * (160 * 1024 / T::kLds);
+        if (tiles > fit) tiles = fit;
+    }
     if (T::kLds > 64 * 1024) {
         const hipError_t e = ask_lds<kernel>(T::kLds);
         if (e != hipSuccess) return e;

@@ -45,7 +45,9 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Problem p, int col_til
     __shared__ w4_f32x4 sums[WAVES][RT * CT][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, col = lane & 15, quad = lane >> 4;
     GroupTile t;
-    if (!find_tile(p.offsets, p.E, p.M, 16 * CT, col_tiles, (int)blockIdx.x, &t)) return;
+    GroupTiles all;
+    all.init(p.offsets, p.E, p.M, 16 * CT, col_tiles);
+    if (!all.find((int)blockIdx.x, &t)) return;
     const int m0 = t.lo + t.m * 16 * CT, rows = min(16 * CT, t.hi - m0), n0 = t.n * RT;     // n0: in sixteens
     const int tiles = (p.N + 15) / 16, steps = (p.K + 127) / 128, per_step = 128 / p.group, groups = steps * per_step;
     const int words = p.group / 32;                    // matrix instructions of a group
