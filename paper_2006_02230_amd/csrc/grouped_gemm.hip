@@ -1,14 +1,13 @@
 // Matrix products grouped by expert, bfloat16 operands, float32 sums: the forward product of the rows of each group with
 // the group's weights, and the gradients of the rows and of the weights.
 //
-// One kernel in three forms.  A workgroup owns a tile BM x BN of one group's result and walks the reduction in stages of 32,
-// four stage buffers in LDS; a wave keeps a tile WM x WN in registers as 16x16 results of v_mfma_f32_16x16x32_bf16.
+// One kernel in three forms.  A workgroup owns a tile BM x BN of one group's result and walks the reduction in stages of 64,
+// two of them in LDS; a wave keeps a tile WM x WN in registers as 16x16 results of v_mfma_f32_16x16x32_bf16.
 // An operand lies in LDS as it lies in memory, in units of eight values (16 bytes):
-//   * reduction innermost (both operands of the forward product, the rows of the gradient of the rows): [row][32]; a lane
-//     reads the eight values of its row that one instruction takes.  The unit c of a row is stored in place
-//     c ^ (-(row / 4) & 3): the 16 lanes that a wide read serves at a time (0-3, 12-15, 20-23, 24-27 and their like) then fall on
-//     different banks, as they do not with c ^ (row / 4 & 3) (twice the cycles).
-//   * reduction outermost (weights in the gradient of the rows, both operands in that of the weights): [32][columns]; the
+//   * reduction innermost (both operands of the forward product, the rows of the gradient of the rows): [row][64]; a lane
+//     reads the eight values of its row that one instruction takes.  The unit c of a row is stored in place c ^ (row & 7), so
+//     that the lanes of one read fall on different banks (counted: no conflicts in any of the forms).
+//   * reduction outermost (weights in the gradient of the rows, both operands in that of the weights): [64][columns]; the
 //     transposing LDS read gives a lane four values of its column from four rows.  Blocks of 16 columns are stored in the
 //     block's place ^ a number of the row that differs for the eight rows that half a wave reads at a time.
 // Loads go from memory into LDS without registers; the permutation is applied to the address a lane loads from.  Lanes past an
@@ -31,8 +30,8 @@ typedef short gg_i16x4 __attribute__((ext_vector_type(4)));
 typedef int gg_i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t gg_u32x2 __attribute__((ext_vector_type(2)));
 
-constexpr int kStage = 32;                          // reduction of a stage: of one matrix instruction
-constexpr int kBuffers = 4;                         // stages in LDS
+constexpr int kStage = 64;                          // reduction of a stage: two matrix instructions' of 32
+constexpr int kBuffers = 2;                         // stages in LDS
 constexpr int kIndices = 4096;                      // row indices of the reduction kept in LDS at a time
 constexpr uint32_t kFarOffset = 0xfffffff0u;        // out of range of every descriptor here
 constexpr uint64_t kFarRecords = 0xffffffe0ull;     // so that no sum of an offset in range and a load's width reaches 2^32
@@ -58,8 +57,8 @@ __device__ __forceinline__ gg_i32x4 gg_rsrc(const char *base, int64_t bytes)
     return gg_i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffffu), (int)(uint32_t)n, 0x00020000};
 }
 // Sixteen bytes a lane into LDS at `lds` + 16 * lane; not waited for.  As assembly, because the compiler puts a wait for every such
-// load before each transposing LDS read, whichever buffer it reads (dX 1050 -> 902, dW 820 -> 512 TFLOP/s at 16384 x 4096 x
-// 2048).  Nothing is written to a register; the waits are gg_wait()'s.  The wait states are those that a descriptor or m0 just written needs; nothing else
+// load before each transposing LDS read, whichever buffer it reads (measured with stages of 32 at 16384 x 4096 x 2048: dX 1112
+// against 902, dW 865 against 512 TFLOP/s).  Nothing is written to a register; the waits are gg_wait()'s.  The wait states are those that a descriptor or m0 just written needs; nothing else
 // in these kernels uses m0.
 __device__ __forceinline__ void gg_dma(gg_i32x4 rsrc, uint32_t lds, uint32_t off)
 {
@@ -128,7 +127,7 @@ struct Operand {
     {
         return R == 64 ? ((kr >> 1) & 1) | ((kr >> 3) & 1) << 1 : (kr & 3) | ((kr >> 3) & 1) << 2;
     }
-    static __device__ __forceinline__ int turn(int r) { return -(r >> 2) & 3; }
+    static __device__ __forceinline__ int turn(int r) { return r & 7; }
     static __device__ __forceinline__ bool mine(int tid) { return kAll >= THREADS || tid < kAll; }
     static __device__ __forceinline__ int lds_row(int tid, int i) { return tid / kRow + i * (THREADS / kRow); }
     // which unit of its row the thread's unit i holds
@@ -215,13 +214,13 @@ struct Operand {
     }
 
     // What one instruction takes of rows r0 .. r0+15.
-    static __device__ __forceinline__ lanes_u32x4 operand(const char *lds, int r0, int lane)
+    static __device__ __forceinline__ lanes_u32x4 operand(const char *lds, int r0, int kk, int lane)
     {
         if constexpr (!RED_OUTER) {
             const int r = r0 + (lane & 15);
-            return *reinterpret_cast<const lanes_u32x4 *>(lds + r * (kStage * 2) + (((lane >> 4) ^ turn(lane & 15)) * 16));
+            return *reinterpret_cast<const lanes_u32x4 *>(lds + r * (kStage * 2) + (((kk * 4 + (lane >> 4)) ^ turn(lane & 15)) * 16));
         } else {
-            const int kr = (lane >> 4) * 8 + ((lane & 15) >> 2);
+            const int kr = kk * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
             const char *at = lds + kr * (R * 2) + ((r0 >> 4) ^ spread(kr)) * 32 + (lane & 3) * 8;
             const gg_u32x2 lo = gg_read_tr(at), hi = gg_read_tr(at + 4 * R * 2);   // spread(kr + 4) == spread(kr) here
             return lanes_u32x4{lo[0], lo[1], hi[0], hi[1]};
@@ -323,12 +322,14 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             return (red + kStage - 1) / kStage;
         }
     };
-    // In step s the matrix cores work on stage s, which is in registers, while stage s+1 is read from LDS and stage s+4 is asked for,
-    // a load between the products of two rows of results, into the buffer that stage s has left.  DMA: three stages are under way
-    // at any time; s+1 is waited for when the loads behind it are all that is left.
-    constexpr int kAhead = T::kDma ? kBuffers : 2, kLoads = T::A::kUnits + T::B::kUnits;
+    // Half a stage is in registers while the matrix cores work on the other half.  In the second half of stage s the first half of
+    // s+1 is read and stage s+2 asked for, into the buffer that s has left: every wave has its last values in registers.  It is waited
+    // for a stage later.  Stages of 32 in four buffers, three under way, were slower where the reduction is
+    // innermost, for the memory then gives half a cache line a row (16384 x 2048 x 4160 forward: 1074 against 1160 TFLOP/s).
+    constexpr int kLoads = T::A::kUnits + T::B::kUnits;
     int *const index = reinterpret_cast<int *>(grouped_lds + kBuffers * T::kStageBytes);
-    const auto buffer = [&](int s) { return grouped_lds + s % kBuffers * T::kStageBytes; };
+    const auto buffer = [&](int s) { return grouped_lds + (s & 1) * T::kStageBytes; };
+    static_assert(kBuffers == 2, "the halves of a stage below");
     const auto load = [&](int s, int i) {
         if (i < T::A::kUnits) A.unit(s, i, buffer(s), tid);
         else B.unit(s, i - T::A::kUnits, buffer(s) + T::A::kBytes, tid);
@@ -343,7 +344,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         A.commit(buffer(s), tid);
         B.commit(buffer(s) + T::A::kBytes, tid);
     };
-    // waits until this wave's loads are down to those of BEHIND stages (or to none), then for the other waves
+    // waits until this wave's loads are down to those of BEHIND stages (DMA) or to none, then for the other waves
     const auto land = [&](auto behind) {
         constexpr int kBehind = T::kDma ? decltype(behind)::value : 0;
         if (T::A::mine(tid) && T::B::mine(tid)) gg_wait<kBehind * kLoads>();
@@ -353,34 +354,40 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         __builtin_amdgcn_sched_barrier(0);
     };
     // the n-th operand of a stage: the columns', then the rows'
-    const auto read = [&](int s, int n, lanes_u32x4 (&a)[MI], lanes_u32x4 (&b)[NI]) {
-        if (n < NI) b[n] = T::B::operand(buffer(s) + T::A::kBytes, wn + n * 16, lane);
-        else a[n - NI] = T::A::operand(buffer(s), wm + (n - NI) * 16, lane);
+    const auto read = [&](int s, int kk, int n, lanes_u32x4 (&a)[MI], lanes_u32x4 (&b)[NI]) {
+        if (n < NI) b[n] = T::B::operand(buffer(s) + T::A::kBytes, wn + n * 16, kk, lane);
+        else a[n - NI] = T::A::operand(buffer(s), wm + (n - NI) * 16, kk, lane);
     };
     gg_f32x4 acc[MI][NI];
-    const auto step = [&](int s, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI], lanes_u32x4 (&b_next)[NI]) {
-        commit(s + 1);
-        land(std::integral_constant<int, kBuffers - 2>{});        // stage s+1; and this wave has what it read of stage s
-        if (T::B::kIndexed && (s + kAhead) % (kIndices / kStage) == 0) {     // the next indices, rarely
-            B.load_indices(index, (s + kAhead) * kStage, tid);
-            __syncthreads();
+    const auto step = [&](int s, auto half, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI],
+                          lanes_u32x4 (&b_next)[NI]) {
+        constexpr bool kSecond = decltype(half)::value;
+        if constexpr (kSecond) {
+            commit(s + 1);
+            land(std::integral_constant<int, 0>{});          // stage s+1; and this wave has what it read of stage s
+            if (T::B::kIndexed && (s + kBuffers) % (kIndices / kStage) == 0) {     // the next indices, rarely
+                B.load_indices(index, (s + kBuffers) * kStage, tid);
+                __syncthreads();
+            }
         }
-        // the reads of the next stage and the loads of a later one between the products: issued in one go, they hold
-        // the matrix cores up while the LDS takes them in
-        constexpr int kReads = MI + NI, kSpread = MI > 2 ? MI - 1 : MI;
+        // The reads of the next half and the loads go between the products: issued in one go, they hold the matrix cores up while the LDS
+        // takes them in.  The loads come early, they have the longest way.
+        constexpr int kReads = MI + NI, kReadRows = MI > 2 ? MI - 1 : MI, kLoadRows = (MI + 1) / 2;
 #pragma unroll
         for (int i = 0; i < MI; ++i) {
             // columns as the instruction's rows: a lane then holds four neighbouring columns of one row of the result
 #pragma unroll
             for (int j = 0; j < NI; ++j) acc[i][j] = gg_mfma(b[j], a[i], acc[i][j]);
-            if (i == 0) {
-                A.begin(s + kAhead, tid);
-                B.begin(s + kAhead, tid);
+            if (kSecond && i == 0) {
+                A.begin(s + kBuffers, tid);
+                B.begin(s + kBuffers, tid);
             }
 #pragma unroll
-            for (int n = i * kReads / kSpread; n < (i + 1) * kReads / kSpread && n < kReads; ++n) read(s + 1, n, a_next, b_next);
+            for (int n = i * kReads / kReadRows; n < (i + 1) * kReads / kReadRows && n < kReads; ++n) read(s + kSecond, !kSecond, n, a_next, b_next);
+            if constexpr (kSecond) {
 #pragma unroll
-            for (int l = i * kLoads / MI; l < (i + 1) * kLoads / MI; ++l) load(s + kAhead, l);
+                for (int l = i * kLoads / kLoadRows; l < (i + 1) * kLoads / kLoadRows && l < kLoads; ++l) load(s + kBuffers, l);
+            }
             __builtin_amdgcn_sched_barrier(0);
         }
     };
@@ -488,11 +495,10 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             lanes_u32x4 a0[MI], b0[NI], a1[MI], b1[NI];
             land(std::integral_constant<int, kBuffers - 1>{});
 #pragma unroll
-            for (int n = 0; n < MI + NI; ++n) read(0, n, a0, b0);
-            for (int s = 0; s < stages; s += 2) {
-                step(s, a0, b0, a1, b1);
-                if (s + 1 >= stages) break;
-                step(s + 1, a1, b1, a0, b0);
+            for (int n = 0; n < MI + NI; ++n) read(0, 0, n, a0, b0);
+            for (int s = 0; s < stages; ++s) {
+                step(s, std::false_type{}, a0, b0, a1, b1);
+                step(s, std::true_type{}, a1, b1, a0, b0);
             }
             land(std::integral_constant<int, 0>{});        // no wave reads the stages any more, no load is under way
         }
