@@ -48,13 +48,15 @@ struct GroupedProblem {
 };
 hipError_t grouped_gemm_launch(const GroupedProblem &p, hipStream_t st);   // hipErrorInvalidValue: no kernel holds it
 
-// w4_kernels.hip: weights in 4 bits, a scale (and a zero point) for `group` inputs of a row.
-struct W4Problem {
+// few_rows.hip: products of few rows, with weights in bfloat16 (w) or in 4 bits, a scale (and a zero point) for `group` inputs of
+// an output.
+struct FewRowsProblem {
     int E, M, N, K, group;
     const int32_t *offsets, *rows;  // offsets NULL: one group of all rows
     int src_rows;
     const uint16_t *x;
     int64_t ldx;
+    const uint16_t *w;              // NULL: in 4 bits
     const uint8_t *q;
     const uint16_t *scales;
     const uint8_t *zeros;           // NULL: 8
@@ -63,7 +65,8 @@ struct W4Problem {
     bool out_f32;
     int act;
 };
-hipError_t w4_launch(const W4Problem &p, hipStream_t st);
+hipError_t few_rows_launch(const FewRowsProblem &p, hipStream_t st);
+// w4_kernels.hip
 hipError_t w4_pack_launch(int E, int N, int K, int group, const uint16_t *w, uint8_t *q, uint16_t *scales, uint8_t *zeros, hipStream_t st);
 
 }  // namespace polydl

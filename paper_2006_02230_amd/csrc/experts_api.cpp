@@ -167,8 +167,8 @@ int polydl_w4_gemm_bf16(int E, int M, int N, int K, int group, const int32_t *of
         return POLYDL_ERR_UNSUPPORTED;
     if (!on_gfx950()) return POLYDL_ERR_NO_DEVICE;
     if (M == 0) return POLYDL_OK;
-    W4Problem p{E, M, N, K, group, offsets, rows, x_rows, x, ldx, q, scales, zeros, y, ldy, out_type == POLYDL_F32, act};
-    return launched_or_refused(w4_launch(p, (hipStream_t)stream));
+    const FewRowsProblem p{E, M, N, K, group, offsets, rows, x_rows, x, ldx, nullptr, q, scales, zeros, y, ldy, out_type == POLYDL_F32, act};
+    return launched_or_refused(few_rows_launch(p, (hipStream_t)stream));
 }
 
 }  // extern "C"

@@ -597,6 +597,11 @@ static hipError_t grouped_pick(const GroupedProblem &q, hipStream_t st)
 
 hipError_t grouped_gemm_launch(const GroupedProblem &q, hipStream_t st)
 {
+    if (q.form == GROUPED_FWD && q.M <= 16 * (int64_t)q.E) {
+        const FewRowsProblem f{q.E, q.M, q.cols, q.red, 0, q.offsets, q.rows, q.src_rows, q.a, q.lda, q.b, nullptr, nullptr, nullptr, q.c, q.ldc,
+                               q.out_f32, q.act};
+        return few_rows_launch(f, st);
+    }
     return q.form == GROUPED_FWD ? grouped_pick<GROUPED_FWD>(q, st)
            : q.form == GROUPED_DX ? grouped_pick<GROUPED_DX>(q, st)
                                   : grouped_pick<GROUPED_DW>(q, st);
