@@ -15,6 +15,7 @@
 // instructions of its own.  Products are exact and the sums float32, taken in the same order, so a group of codes that equal the zero
 // point gives exactly zero; otherwise both are rounded as sums of terms of up to 31 |x| are.
 #include <hip/hip_runtime.h>
+#include <type_traits>
 #include "experts.hpp"
 #include "group_tiles.hpp"
 #include "internal.hpp"
@@ -35,9 +36,12 @@ __device__ __forceinline__ few_f32x4 few_mfma(lanes_u32x4 a, lanes_u32x4 b, few_
     return c;
 #endif
 }
-// eight values at k of a row of K, zeros past its end
+// Eight values at k of a row of K, zeros past its end.  WHOLE: the step that k lies in ends inside the row, which is the wave's
+// to know and costs its lanes nothing.
+template <bool WHOLE>
 __device__ __forceinline__ lanes_u32x4 few_row(const uint16_t *row, int k, int K)
 {
+    if constexpr (WHOLE) return load_unit8(row + k);
     return k < K ? load_unit8(row + k, K - k) : lanes_u32x4{0u, 0u, 0u, 0u};
 }
 
@@ -46,16 +50,18 @@ struct WholeWeights {
     static constexpr int kStep = 64, kOps = 2;
     struct Held { lanes_u32x4 v[kOps]; };
     static __device__ __forceinline__ int input(int i, int quad) { return quad * 16 + i * 8; }
-    const FewRowsProblem &p;
-    const uint16_t *row;           // of the lane's output
+    const uint16_t *row;           // of the lane's output, its inputs of step 0
 
-    __device__ __forceinline__ WholeWeights(const FewRowsProblem &p_, int e, int tile, int, int lane)
-        : p(p_), row(p_.w + ((int64_t)e * p_.N + min(tile * 16 + (lane & 15), p_.N - 1)) * p_.K) {}
-    __device__ __forceinline__ Held load(int s, int lane) const
+    __device__ __forceinline__ void init(const FewRowsProblem &p, int e, int tile, int lane)
+    {
+        row = p.w + ((int64_t)e * p.N + min(tile * 16 + (lane & 15), p.N - 1)) * p.K;
+    }
+    template <bool WHOLE>
+    __device__ __forceinline__ Held load(int s, int K, int lane) const
     {
         Held h;
 #pragma unroll
-        for (int i = 0; i < kOps; ++i) h.v[i] = few_row(row, s * kStep + input(i, lane >> 4), p.K);
+        for (int i = 0; i < kOps; ++i) h.v[i] = few_row<WHOLE>(row, s * kStep + input(i, lane >> 4), K);
         return h;
     }
     template <int CT>
@@ -68,40 +74,44 @@ struct WholeWeights {
     }
 };
 
-// GROUP: inputs of a scale.
-template <int GROUP>
+// GROUP: inputs of a scale.  ZEROS: there are zero points (a test at run time would make the wave wait for each as it is loaded:
+// 32 rows of 64 experts, 2048 x 4096, 48 us against 34).
+template <int GROUP, bool ZEROS>
 struct CodedWeights {
     static constexpr int kStep = 128, kOps = 4, kGroups = kStep / GROUP, kOpsGroup = kOps / kGroups;
     struct Held { lanes_u32x4 q; few_u32x2 scale[kGroups]; uint32_t zero[kGroups]; };
     static __device__ __forceinline__ int input(int i, int quad) { return i * 32 + quad * 8; }
-    const uint8_t *q;              // of the lane, step 0
-    const uint16_t *scales;        // of the lane's four outputs of the result, group 0
-    const uint8_t *zeros;          // of the lane's output among the operands; NULL: 8
+    // of the tile, step 0 (the same for the wave, so that only 32-bit offsets are the lanes'); no zeros: 8
+    const uint8_t *q, *zeros;
+    const uint16_t *scales;
 
-    __device__ __forceinline__ CodedWeights(const FewRowsProblem &p, int e, int tile, int tiles, int lane)
+    __device__ __forceinline__ void init(const FewRowsProblem &p, int e, int tile, int)
     {
-        const int steps = (p.K + kStep - 1) / kStep;
-        const int64_t at = (int64_t)e * tiles + min(tile, tiles - 1);
-        q = p.q + (at * steps * 64 + lane) * 16;
-        scales = p.scales + at * steps * kGroups * 16 + (lane >> 4) * 4;
-        zeros = p.zeros ? p.zeros + at * steps * kGroups * 16 + (lane & 15) : nullptr;
+        const int tiles = (p.N + 15) / 16, steps = (p.K + kStep - 1) / kStep;
+        const int64_t at = ((int64_t)e * tiles + min(tile, tiles - 1)) * steps;
+        q = p.q + at * 1024;
+        scales = p.scales + at * (kGroups * 16);
+        zeros = ZEROS ? p.zeros + at * (kGroups * 16) : nullptr;
     }
-    __device__ __forceinline__ Held load(int s, int) const
+    template <bool WHOLE>
+    __device__ __forceinline__ Held load(int s, int, int lane) const
     {
         Held h;
-        h.q = *reinterpret_cast<const lanes_u32x4 *>(q + (int64_t)s * 1024);
+        h.q = *reinterpret_cast<const lanes_u32x4 *>(q + (int64_t)s * 1024 + (uint32_t)lane * 16u);
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
             const int64_t at = ((int64_t)s * kGroups + g) * 16;
-            h.scale[g] = *reinterpret_cast<const few_u32x2 *>(scales + at);
-            h.zero[g] = zeros ? zeros[at] : 8u;
+            h.scale[g] = *reinterpret_cast<const few_u32x2 *>(scales + at + (uint32_t)(lane >> 4) * 4u);   // of four outputs of the result
+            h.zero[g] = ZEROS ? zeros[at + (uint32_t)(lane & 15)] : 8u;                                    // of an output among the operands
         }
         return h;
     }
     // eight codes as 16 + q, in the order of the inputs
     static __device__ __forceinline__ lanes_u32x4 codes(uint32_t w)
     {
-        constexpr uint32_t mask = 0x00780078u, sixteen = 0x41804180u;
+        // in registers: the and-or has no room for constants, and as constants they are two instructions
+        uint32_t mask = 0x00780078u, sixteen = 0x41804180u;
+        asm("" : "+v"(mask), "+v"(sixteen));
         return lanes_u32x4{((w << 3) & mask) | sixteen, ((w >> 1) & mask) | sixteen, ((w >> 5) & mask) | sixteen, ((w >> 9) & mask) | sixteen};
     }
     template <int CT>
@@ -132,8 +142,8 @@ struct CodedWeights {
     }
 };
 
-// WAVES waves share a tile of 16 outputs * RT by 16 rows * CT; STEPS steps of a wave are under way at a time.
-template <class W, int RT, int CT, int WAVES, int STEPS, bool OUT_F32>
+// WAVES waves share a tile of 16 outputs * RT by 16 rows * CT.
+template <class W, int RT, int CT, int WAVES, bool OUT_F32>
 __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsProblem p, int col_tiles)
 {
     __shared__ few_f32x4 sums[WAVES][RT * CT][64];
@@ -162,35 +172,32 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsProblem p, 
 #pragma unroll
         for (int c = 0; c < CT; ++c) total[r][c] = few_f32x4{0.f, 0.f, 0.f, 0.f};
 
-    for (int s0 = wave; s0 < steps; s0 += WAVES * STEPS) {
-        typename W::Held w[STEPS][RT];
-        lanes_u32x4 xv[STEPS][CT][W::kOps];
+    W weights[RT];
+    if (steps > 0) {
 #pragma unroll
-        for (int u = 0; u < STEPS; ++u) {
-            const int s = s0 + u * WAVES;
-            if (s >= steps) continue;
-#pragma unroll
-            for (int r = 0; r < RT; ++r) w[u][r] = W(p, t.e, n0 + r, (p.N + 15) / 16, lane).load(s, lane);
-        }
-#pragma unroll
-        for (int u = 0; u < STEPS; ++u) {
-            const int s = s0 + u * WAVES;
-            if (s >= steps) continue;
-#pragma unroll
-            for (int c = 0; c < CT; ++c)
-#pragma unroll
-                for (int i = 0; i < W::kOps; ++i) {
-                    xv[u][c][i] = lanes_u32x4{0u, 0u, 0u, 0u};
-                    if (x[c]) xv[u][c][i] = few_row(x[c], s * W::kStep + W::input(i, quad), p.K);
-                }
-        }
-#pragma unroll
-        for (int u = 0; u < STEPS; ++u) {
-            if (s0 + u * WAVES >= steps) continue;
-#pragma unroll
-            for (int r = 0; r < RT; ++r) W(p, t.e, n0 + r, (p.N + 15) / 16, lane).template multiply<CT>(w[u][r], xv[u], total[r]);
-        }
+        for (int r = 0; r < RT; ++r) weights[r].init(p, t.e, n0 + r, lane);
     }
+    const auto step = [&](int s, auto whole) {
+        typename W::Held w[RT];
+        lanes_u32x4 xv[CT][W::kOps];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) w[r] = weights[r].template load<decltype(whole)::value>(s, p.K, lane);
+#pragma unroll
+        for (int c = 0; c < CT; ++c) {
+#pragma unroll
+            for (int i = 0; i < W::kOps; ++i) xv[c][i] = lanes_u32x4{0u, 0u, 0u, 0u};
+            if (x[c]) {
+#pragma unroll
+                for (int i = 0; i < W::kOps; ++i) xv[c][i] = few_row<decltype(whole)::value>(x[c], s * W::kStep + W::input(i, quad), p.K);
+            }
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) weights[r].template multiply<CT>(w[r], xv, total[r]);
+    };
+    const int whole_steps = min(steps, p.K / W::kStep);
+    int s = wave;
+    for (; s < whole_steps; s += WAVES) step(s, std::true_type{});
+    if (s < steps) step(s, std::false_type{});
 
 #pragma unroll
     for (int r = 0; r < RT; ++r)
@@ -233,32 +240,41 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsProblem p, 
     }
 }
 
-template <class W, int RT, int CT, int WAVES, int STEPS>
+template <class W, int RT, int CT, int WAVES>
 static hipError_t few_rows_run(const FewRowsProblem &p, hipStream_t st)
 {
     const int64_t groups = p.M < p.E + 1 ? p.M : p.E + 1, col_tiles = ((p.N + 15) / 16 + RT - 1) / RT;
     const int64_t tiles = (p.M + groups * (16 * CT - 1)) / (16 * CT) * col_tiles;
     if (tiles > 0x7fffffff) return hipErrorInvalidValue;
     if (p.out_f32)
-        return launch_kernel((few_rows_kernel<W, RT, CT, WAVES, STEPS, true>), dim3((unsigned)tiles), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
-    return launch_kernel((few_rows_kernel<W, RT, CT, WAVES, STEPS, false>), dim3((unsigned)tiles), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
+        return launch_kernel((few_rows_kernel<W, RT, CT, WAVES, true>), dim3((unsigned)tiles), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
+    return launch_kernel((few_rows_kernel<W, RT, CT, WAVES, false>), dim3((unsigned)tiles), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
 }
 
-template <class W, int STEPS>
+template <class W>
 static hipError_t few_rows_pick(const FewRowsProblem &p, hipStream_t st)
 {
     const int rows = (p.M + p.E - 1) / p.E;            // of a group, in the mean
-    if (rows <= 16) return few_rows_run<W, 1, 1, 8, STEPS>(p, st);
-    if (rows <= 32) return few_rows_run<W, 2, 2, 8, 1>(p, st);
-    return few_rows_run<W, 2, 4, 8, 1>(p, st);
+    if (rows <= 16) {
+        // Two tiles of outputs share the rows' loads; with fewer workgroups than compute units that costs more than it saves (one row, 4096 x
+        // 4096 in 4 bits: 4.6 us with one tile, 5.5 with two; 32 rows of 64 experts, 2048 x 4096: 38 and 34).  Four waves take longer over a
+        // tile than eight, and more workgroups fit at a time (those 32 rows: 31 us; 16 rows, 8192 x 8192: 13.4 against 13.1).
+        const int64_t chunks = p.M < p.E ? p.M : p.E, tiles = chunks * ((p.N + 31) / 32), cus = compute_units();
+        return tiles < cus ? few_rows_run<W, 1, 1, 8>(p, st) : tiles < 4 * cus ? few_rows_run<W, 2, 1, 8>(p, st) : few_rows_run<W, 2, 1, 4>(p, st);
+    }
+    return rows <= 32 ? few_rows_run<W, 2, 2, 8>(p, st) : few_rows_run<W, 2, 4, 8>(p, st);
+}
+
+template <int GROUP>
+static hipError_t few_rows_coded(const FewRowsProblem &p, hipStream_t st)
+{
+    return p.zeros ? few_rows_pick<CodedWeights<GROUP, true>>(p, st) : few_rows_pick<CodedWeights<GROUP, false>>(p, st);
 }
 
 hipError_t few_rows_launch(const FewRowsProblem &p, hipStream_t st)
 {
-    if (p.w) return few_rows_pick<WholeWeights, 4>(p, st);
-    return p.group == 32   ? few_rows_pick<CodedWeights<32>, 4>(p, st)
-           : p.group == 64 ? few_rows_pick<CodedWeights<64>, 4>(p, st)
-                           : few_rows_pick<CodedWeights<128>, 4>(p, st);
+    if (p.w) return few_rows_pick<WholeWeights>(p, st);
+    return p.group == 32 ? few_rows_coded<32>(p, st) : p.group == 64 ? few_rows_coded<64>(p, st) : few_rows_coded<128>(p, st);
 }
 
 }  // namespace polydl

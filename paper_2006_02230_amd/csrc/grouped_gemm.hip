@@ -250,7 +250,7 @@ struct GroupedTile {
     // The workgroups of the forward product and of the gradient of the rows, whose tiles are alike, take tile after tile; those of the gradient of
     // the weights take one each, as the groups' lengths come, and their results leave through the stages' LDS.
     static constexpr bool kLoops = FORM != GROUPED_DW;
-    static constexpr int kOutAt = kLoops ? kBuffers * kStageBytes : 0, kOutBytes = kLoops ? kThreads / 64 * 4096 : kBuffers * kStageBytes;
+    static constexpr int kOutAt = kLoops ? kBuffers * kStageBytes : 0, kOutBytes = kThreads / 64 * 4096;
     static constexpr int kLds = kLoops ? kOutAt + kOutBytes : kBuffers * kStageBytes + kIndexBytes;
 };
 
@@ -586,17 +586,37 @@ static bool grouped_whole_units(const GroupedProblem &q, int bm, int bn)
     return q.out_rows % 8 == 0 && kStage * q.lda * 2 < last && (q.rows ? (int64_t)q.src_rows : (int64_t)kStage) * q.ldb * 2 < last;
 }
 
+// Tiles of 256 x 256, one workgroup on a compute unit, or of 128 x 128, two: what is left of the last round decides.  A round of
+// the small ones takes 0.65 of a round of the large ones and does half the work (4096 x 4096 x 4096: 117 us in one round of 256, 155 in two of
+// 128).  Tiles are counted for groups of the mean length, each with half a tile more.  Measured both ways, forward, us for 256 / 128: 16 groups of 256
+// rows, 2048 x 2048, 66 / 80; of 400, 99 / 95; of 1024, 176 / 200; one of 4096, 57 / 42.  Up to 128 rows a group the large tiles
+// are mostly empty (16 groups of 128: 62 / 52).  Weight gradients of few tiles a group need the small ones to even the groups out (64 groups of 512 rows, 512 x
+// 512: 74 / 55; 8 of 1024 rows, 1024 x 2048: 51 / 56).
+template <int FORM>
+static bool grouped_large_tiles(const GroupedProblem &q)
+{
+    const int64_t cus = compute_units();
+    const auto rounds = [&](int64_t tile, int64_t at_a_time) {
+        const int64_t across = (q.cols + tile - 1) / tile;
+        const int64_t down = FORM == GROUPED_DW ? (q.out_rows + tile - 1) / tile * q.E
+                             : q.E == 1         ? (q.M + tile - 1) / tile
+                                                : (q.M + q.E * (tile / 2)) / tile;
+        return (across * down + at_a_time - 1) / at_a_time;
+    };
+    if (FORM == GROUPED_DW ? ((int64_t)q.out_rows + 255) / 256 * ((q.cols + 255) / 256) < 8 : q.M <= 128 * (int64_t)q.E) return false;
+    return (double)rounds(256, cus) <= 0.65 * (double)rounds(128, 2 * cus);
+}
+
 template <int FORM>
 static hipError_t grouped_pick(const GroupedProblem &q, hipStream_t st)
 {
     if (!grouped_whole_units(q, 256, 256)) return grouped_pick_types<FORM, 128, 128, 64, 64, false>(q, st);
-    const int64_t rows = FORM == GROUPED_DW ? q.out_rows : q.M / q.E;    // of a group, in the mean
-    if (rows > 128) return grouped_pick_types<FORM, 256, 256, 128, 64, true>(q, st);
-    return grouped_pick_types<FORM, 128, 128, 64, 64, true>(q, st);
+    return grouped_large_tiles<FORM>(q) ? grouped_pick_types<FORM, 256, 256, 128, 64, true>(q, st) : grouped_pick_types<FORM, 128, 128, 64, 64, true>(q, st);
 }
 
 hipError_t grouped_gemm_launch(const GroupedProblem &q, hipStream_t st)
 {
+    // up to 16 rows a group in the mean (8 groups of 4096 x 4096, few rows / tiles of 128: 20 rows 75 / 81 us, 32 rows 94 / 81)
     if (q.form == GROUPED_FWD && q.M <= 16 * (int64_t)q.E) {
         const FewRowsProblem f{q.E, q.M, q.cols, q.red, 0, q.offsets, q.rows, q.src_rows, q.a, q.lda, q.b, nullptr, nullptr, nullptr, q.c, q.ldc,
                                q.out_f32, q.act};
