@@ -45,6 +45,29 @@ __device__ __forceinline__ float lane_of(float x, int lane)
     return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
 }
 
+// Over LANES neighbouring lanes, 16 (a row: four rotations) or 64, the result in all of them.
+#define POLYDL_ROW_STEPS(STEP) STEP(0x128) STEP(0x124) STEP(0x122) STEP(0x121)
+template <int LANES>
+__device__ __forceinline__ uint32_t group_max(uint32_t x)
+{
+    if constexpr (LANES == 64) return wave_max(x);
+#define STEP(C) { const uint32_t o = (uint32_t)dpp_of<C, 0xf>(0, (int)x); x = o > x ? o : x; }
+    POLYDL_ROW_STEPS(STEP)
+#undef STEP
+    return x;
+}
+template <int LANES>
+__device__ __forceinline__ uint32_t group_min(uint32_t x) { return ~group_max<LANES>(~x); }
+template <int LANES>
+__device__ __forceinline__ float group_sum(float x)
+{
+    if constexpr (LANES == 64) return wave_sum(x);
+#define STEP(C) x += __builtin_bit_cast(float, dpp_of<C, 0xf>(0, __builtin_bit_cast(int, x)));
+    POLYDL_ROW_STEPS(STEP)
+#undef STEP
+    return x;
+}
+
 // bfloat16 bits <-> float.  To bfloat16: round to nearest, ties to even; the compiler's conversion is one instruction a pair.
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __builtin_bit_cast(float, w & 0xffff0000u); }

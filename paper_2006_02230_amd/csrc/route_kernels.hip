@@ -1,12 +1,13 @@
 // The router of a layer of experts, its plan and its gradient, and the weighted sum over a token's experts.
 //
 // route: of each token's E logits the k largest (ties: the lowest index; logits of -infinity never), their softmax
-// weights, and the slots sorted by expert that the grouped products work on.  One wave takes a token: a lane holds E/64 logits as
-// ordered unsigned keys, a round is a maximum over the wave and the removal of one key, so the order does not depend on
-// rounding and a tie is settled by a ballot.  64 tokens make a workgroup; each expert's tokens there are a mask of 64 bits in
-// LDS, set with atomic ORs: a slot's place inside its expert is the number of bits below its own, the same in every run.
-// Bound: latency.  The logits of 16384 tokens and 128 experts are 8 MB, 1.5 us of HBM; a round is a chain of about 20
-// dependent instructions.
+// weights, and the slots sorted by expert that the grouped products work on.  16 lanes take a token of up to 256 experts, four tokens a
+// wave, and a wave one of more; a lane holds E/16 or E/64 logits as ordered unsigned keys.  A round is a maximum over the lanes, the lowest
+// index that has it, and that key's removal, so the order does not depend on rounding.  64 tokens make a workgroup; each
+// expert's tokens there are a mask of 64 bits in LDS, set with atomic ORs: a slot's place inside its expert is the number of
+// bits below its own, the same in every run.
+// Bound: instruction issue and latency.  The logits of 16384 tokens and 128 experts are 8 MB, 1.5 us of HBM; a round of four tokens is 50
+// instructions of which 20 wait for one another.  16384 tokens, 128 experts, 8 choices: 7.6 us (13.6 with a wave to a token).
 #include <hip/hip_runtime.h>
 #include <math.h>
 #include "experts.hpp"
@@ -28,52 +29,64 @@ __device__ __forceinline__ float route_value(uint32_t key)
     return __builtin_bit_cast(float, key >> 31 ? key ^ 0x80000000u : ~key);
 }
 
-struct RouteRow { int id; float w; };   // lane j: the j-th choice, -1 and 0 where there is none
+// Lane l of a token's LANES: choices l and l + LANES, -1 and 0 where there is none.
+template <int LANES>
+struct RouteRow {
+    static constexpr int kHeld = LANES < kRouteMaxChoices ? kRouteMaxChoices / LANES : 1;
+    int id[kHeld];
+    float w[kHeld];
+};
 
-template <int NV>
-__device__ __forceinline__ RouteRow route_row(const float *row, int E, int k, bool renorm, int lane)
+// `row`: the token's logits, or NULL for lanes without a token.
+template <int LANES, int NV>
+__device__ __forceinline__ RouteRow<LANES> route_row(const float *row, int E, int k, bool renorm, int l)
 {
+    using Row = RouteRow<LANES>;
     float v[NV];
     uint32_t key[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int e = i * 64 + lane;
-        v[i] = e < E ? row[e] : -INFINITY;
+        const int e = i * LANES + l;
+        v[i] = row && e < E ? row[e] : -INFINITY;
         key[i] = route_key(v[i]);
     }
-    RouteRow r{-1, 0.f};
-    float best = 0.f, mine = 0.f;
+    Row r;
+    float own[Row::kHeld], best = 0.f;
+#pragma unroll
+    for (int h = 0; h < Row::kHeld; ++h) { r.id[h] = -1; r.w[h] = own[h] = 0.f; }
     for (int j = 0; j < k; ++j) {
         uint32_t m = key[0];
 #pragma unroll
         for (int i = 1; i < NV; ++i) m = key[i] > m ? key[i] : m;
-        m = wave_max(m);
-        if (m == 0u) break;                              // nothing left that is not masked
-        int e = -1;
+        m = group_max<LANES>(m);
+        if (!__any(m != 0u)) break;                      // nothing left that is not masked
+        uint32_t e = 0xffffffffu;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            if (e >= 0) continue;
-            const unsigned long long there = __ballot(key[i] == m);
-            if (there) {
-                const int l = __builtin_ctzll(there);
-                e = i * 64 + l;
-                if (lane == l) key[i] = 0u;
-            }
-        }
+        for (int i = NV - 1; i >= 0; --i) e = key[i] == m ? (uint32_t)(i * LANES + l) : e;
+        e = group_min<LANES>(e);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) key[i] = (uint32_t)(i * LANES + l) == e ? 0u : key[i];
         const float x = route_value(m);
         if (j == 0) best = x;
-        if (lane == j) { r.id = e; mine = x; }
-    }
-    if (lane_of(r.id, 0) < 0) return r;                  // every logit masked
-    float sum = 0.f;
-    const float own = r.id >= 0 ? expf(mine - best) : 0.f;
-    if (renorm) {
-        sum = own;
-    } else {
 #pragma unroll
-        for (int i = 0; i < NV; ++i) sum += expf(v[i] - best);
+        for (int h = 0; h < Row::kHeld; ++h)
+            if (h * LANES + l == j && m != 0u) { r.id[h] = (int)e; own[h] = x; }
     }
-    r.w = own / wave_sum(sum);
+    const bool any = group_max<LANES>((uint32_t)(r.id[0] + 1)) != 0u;      // some logit is not masked
+    float sum = 0.f;
+#pragma unroll
+    for (int h = 0; h < Row::kHeld; ++h) {
+        own[h] = r.id[h] >= 0 ? expf(own[h] - best) : 0.f;
+        sum += own[h];
+    }
+    if (!renorm) {
+        sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) sum += any ? expf(v[i] - best) : 0.f;
+    }
+    sum = group_sum<LANES>(sum);
+#pragma unroll
+    for (int h = 0; h < Row::kHeld; ++h) r.w[h] = r.id[h] >= 0 ? own[h] / sum : 0.f;
     return r;
 }
 
@@ -128,24 +141,27 @@ __device__ __forceinline__ void route_place(const RouteProblem &p, const int *id
 }
 
 // Choices of 64 tokens.  ONE: they are all there are, and the plan is made here too; else the counts go to `hist`.
-template <int NV, bool ONE>
+template <int LANES, int NV, bool ONE>
 __global__ __launch_bounds__(1024) void route_choose_kernel(RouteArgs a)
 {
-    __shared__ uint32_t masks[2 * 64 * NV];
-    __shared__ int count[ONE ? 64 * NV : 1], base[ONE ? 64 * NV + 1 : 1], part[16], ids[ONE ? kRouteTokens * kRouteMaxChoices : 1];
+    __shared__ uint32_t masks[2 * LANES * NV];
+    __shared__ int count[ONE ? LANES * NV : 1], base[ONE ? LANES * NV + 1 : 1], part[16], ids[ONE ? kRouteTokens * kRouteMaxChoices : 1];
     const RouteProblem &p = a.p;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, waves = blockDim.x >> 6;
+    const int tid = threadIdx.x, l = tid % LANES;
     const int t0 = blockIdx.x * kRouteTokens, nt = min(kRouteTokens, p.T - t0);
-    for (int i = tid; i < 2 * p.E; i += blockDim.x) masks[i] = 0u;
+    for (int i = tid; i < 2 * p.E; i += 1024) masks[i] = 0u;
     __syncthreads();
-    for (int t = wave; t < nt; t += waves) {
-        const RouteRow r = route_row<NV>(p.logits + (size_t)(t0 + t) * p.E, p.E, p.k, p.renorm, lane);
-        if (lane < p.k) {
-            const size_t at = (size_t)(t0 + t) * p.k + lane;
-            p.ids[at] = r.id;
-            p.weights[at] = r.w;
-            if (ONE) ids[t * p.k + lane] = r.id;
-            if (r.id >= 0) atomicOr(&masks[2 * r.id + (t >> 5)], 1u << (t & 31));
+    for (int t = tid / LANES; t < kRouteTokens; t += 1024 / LANES) {
+        const auto r = route_row<LANES, NV>(t < nt ? p.logits + (size_t)(t0 + t) * p.E : nullptr, p.E, p.k, p.renorm, l);
+#pragma unroll
+        for (int h = 0; h < RouteRow<LANES>::kHeld; ++h) {
+            const int j = h * LANES + l;
+            if (t >= nt || j >= p.k) continue;
+            const size_t at = (size_t)(t0 + t) * p.k + j;
+            p.ids[at] = r.id[h];
+            p.weights[at] = r.w[h];
+            if (ONE) ids[t * p.k + j] = r.id[h];
+            if (r.id[h] >= 0) atomicOr(&masks[2 * r.id[h] + (t >> 5)], 1u << (t & 31));
         }
     }
     __syncthreads();
@@ -158,7 +174,7 @@ __global__ __launch_bounds__(1024) void route_choose_kernel(RouteArgs a)
         for (int s = base[p.E] + tid; s < nt * p.k; s += 1024) p.tokens[s] = -1;
     } else {
         const int pad = blockIdx.x == gridDim.x - 1 ? a.pitch - a.blocks : 0;   // the bytes behind a row's end are zero too
-        for (int e = tid; e < p.E; e += blockDim.x) {
+        for (int e = tid; e < p.E; e += 1024) {
             uint8_t *h = a.hist + (size_t)e * a.pitch + blockIdx.x;
             h[0] = (uint8_t)(__builtin_popcount(masks[2 * e]) + __builtin_popcount(masks[2 * e + 1]));
             for (int i = 1; i <= pad; ++i) h[i] = 0;
@@ -246,11 +262,11 @@ size_t route_workspace_bytes(int T, int E)
 // Every workgroup reading all counts saves the scan's launch; its traffic grows with the square of the workgroups.
 constexpr int64_t kRouteRereadBytes = 32ll << 20;
 
-template <int NV>
-static hipError_t route_choose(const RouteArgs &a, bool one, int threads, hipStream_t st)
+template <int LANES, int NV>
+static hipError_t route_choose(const RouteArgs &a, hipStream_t st)
 {
-    if (one) return launch_kernel((route_choose_kernel<NV, true>), dim3(1), dim3(1024), 0, st, a);
-    return launch_kernel((route_choose_kernel<NV, false>), dim3((unsigned)a.blocks), dim3((unsigned)threads), 0, st, a);
+    if (a.blocks <= 1) return launch_kernel((route_choose_kernel<LANES, NV, true>), dim3(1), dim3(1024), 0, st, a);
+    return launch_kernel((route_choose_kernel<LANES, NV, false>), dim3((unsigned)a.blocks), dim3(1024), 0, st, a);
 }
 
 hipError_t route_launch(const RouteProblem &p, void *workspace, hipStream_t st)
@@ -263,11 +279,14 @@ hipError_t route_launch(const RouteProblem &p, void *workspace, hipStream_t st)
         a.before = reinterpret_cast<int32_t *>(a.hist + (((size_t)p.E * a.pitch + 255) & ~(size_t)255));
         a.total = a.before + (size_t)p.E * a.blocks;
     }
-    hipError_t e = p.E <= 64    ? route_choose<1>(a, one, 1024, st)
-                   : p.E <= 128 ? route_choose<2>(a, one, 1024, st)
-                   : p.E <= 256 ? route_choose<4>(a, one, 1024, st)
-                   : p.E <= 512 ? route_choose<8>(a, one, 1024, st)
-                                : route_choose<16>(a, one, 1024, st);
+    auto *choose = p.E <= 16    ? route_choose<16, 1>
+                   : p.E <= 32  ? route_choose<16, 2>
+                   : p.E <= 64  ? route_choose<16, 4>
+                   : p.E <= 128 ? route_choose<16, 8>
+                   : p.E <= 256 ? route_choose<16, 16>
+                   : p.E <= 512 ? route_choose<64, 8>
+                                : route_choose<64, 16>;
+    hipError_t e = choose(a, st);
     if (e != hipSuccess || one) return e;
     if ((int64_t)a.blocks * a.pitch * p.E <= kRouteRereadBytes)
         return launch_kernel(route_place_kernel<false>, dim3((unsigned)a.blocks), dim3(1024), 0, st, a);
@@ -277,88 +296,100 @@ hipError_t route_launch(const RouteProblem &p, void *workspace, hipStream_t st)
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
-// One wave a token.  Weights from the softmax over all experts: dl_e = p_e (g_e - sum_j p_j g_j), g zero where e was not
-// chosen; renormalised: the same with the weights in p's place, zero elsewhere (their logits are not read).
-template <int NV, bool RENORM>
+// Weights from the softmax over all experts: dl_e = p_e (g_e - sum_j p_j g_j), g zero where e was not chosen; renormalised:
+// the same with the weights in p's place, zero elsewhere (their logits are not read).  LANES lanes a token, as in the choice.
+template <int LANES, int NV, bool RENORM>
 __global__ __launch_bounds__(256) void route_bwd_kernel(int T, int E, int k, const float *logits, const int32_t *ids, const float *weights,
                                                         const float *dweights, float *dlogits)
 {
-    const int64_t t = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int lane = threadIdx.x & 63;
-    if (t >= T) return;
-    int id = -1;
-    float g = 0.f, p_own = 0.f;
-    if (lane < k) {
-        id = ids[t * k + lane];
-        id = (unsigned)id < (unsigned)E ? id : -1;
-        if (id >= 0) {
-            g = dweights[t * k + lane];
-            if (RENORM) p_own = weights[t * k + lane];
-        }
+    constexpr int kHeld = RouteRow<LANES>::kHeld;
+    const int l = threadIdx.x % LANES, first = (threadIdx.x & 63) - l;
+    const int64_t t = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const bool here = t < T;
+    int id[kHeld];
+    float g[kHeld], w[kHeld], p[NV], own[NV];
+#pragma unroll
+    for (int h = 0; h < kHeld; ++h) {
+        const int j = h * LANES + l;
+        id[h] = here && j < k ? ids[t * k + j] : -1;
+        if ((unsigned)id[h] >= (unsigned)E) id[h] = -1;
+        g[h] = id[h] >= 0 ? dweights[t * k + j] : 0.f;
+        w[h] = RENORM && id[h] >= 0 ? weights[t * k + j] : 0.f;
     }
-    float p[NV];
     if constexpr (!RENORM) {
         const float *row = logits + t * E;
         float v[NV];
         uint32_t m = 0u;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            const int e = i * 64 + lane;
-            v[i] = e < E ? row[e] : -INFINITY;
+            const int e = i * LANES + l;
+            v[i] = here && e < E ? row[e] : -INFINITY;
             const uint32_t key = route_key(v[i]);
             m = key > m ? key : m;
         }
-        m = wave_max(m);
+        m = group_max<LANES>(m);
         const float best = route_value(m);
         float sum = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
-            p[i] = m ? expf(v[i] - best) : 0.f;
+            p[i] = m ? expf(v[i] - best) : 0.f;          // a row without an open expert has no probabilities
             sum += p[i];
         }
-        sum = m ? wave_sum(sum) : 1.f;
+        sum = group_sum<LANES>(sum);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) p[i] /= sum;
-        if (id >= 0) p_own = m ? expf(row[id] - best) / sum : 0.f;
-    }
-    const float mean = wave_sum(id >= 0 ? p_own * g : 0.f);
-    float own[NV];                                        // the gradient of each lane's weights
+        for (int i = 0; i < NV; ++i) p[i] = m ? p[i] / sum : 0.f;
+    } else {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) {
-        own[i] = 0.f;
-        if (RENORM) p[i] = 0.f;
+        for (int i = 0; i < NV; ++i) p[i] = 0.f;
     }
+#pragma unroll
+    for (int i = 0; i < NV; ++i) own[i] = 0.f;
     for (int j = 0; j < k; ++j) {
-        const int e = lane_of(id, j);
-        const float gj = lane_of(g, j), pj = RENORM ? lane_of(p_own, j) : 0.f;
+        int e = id[0];
+        float gj = g[0], wj = w[0];
+        if (kHeld > 1 && j >= LANES) { e = id[kHeld - 1]; gj = g[kHeld - 1]; wj = w[kHeld - 1]; }
+        const int from = first + j % LANES;
+        e = __shfl(e, from);
+        gj = __shfl(gj, from);
+        if (RENORM) wj = __shfl(wj, from);
 #pragma unroll
         for (int i = 0; i < NV; ++i)
-            if (i * 64 + lane == e) {
+            if (i * LANES + l == e) {
                 own[i] += gj;
-                if (RENORM) p[i] = pj;
+                if (RENORM) p[i] = wj;
             }
     }
+    float mean = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) mean += own[i] != 0.f ? p[i] * own[i] : 0.f;
+    mean = group_sum<LANES>(mean);
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int e = i * 64 + lane;
-        if (e < E) dlogits[t * E + e] = p[i] * (own[i] - mean);
+        const int e = i * LANES + l;
+        if (here && e < E) dlogits[t * E + e] = p[i] * (own[i] - mean);
     }
 }
 
-template <int NV>
+template <int LANES, int NV>
 static hipError_t route_bwd(int T, int E, int k, const float *logits, const int32_t *ids, const float *weights, const float *dweights,
                             bool renorm, float *dlogits, hipStream_t st)
 {
-    const dim3 grid((unsigned)(((int64_t)T + 3) / 4));
+    const dim3 grid((unsigned)(((int64_t)T + 256 / LANES - 1) / (256 / LANES)));
     if (renorm)
-        return launch_kernel((route_bwd_kernel<NV, true>), grid, dim3(256), 0, st, T, E, k, logits, ids, weights, dweights, dlogits);
-    return launch_kernel((route_bwd_kernel<NV, false>), grid, dim3(256), 0, st, T, E, k, logits, ids, weights, dweights, dlogits);
+        return launch_kernel((route_bwd_kernel<LANES, NV, true>), grid, dim3(256), 0, st, T, E, k, logits, ids, weights, dweights, dlogits);
+    return launch_kernel((route_bwd_kernel<LANES, NV, false>), grid, dim3(256), 0, st, T, E, k, logits, ids, weights, dweights, dlogits);
 }
 
 hipError_t route_bwd_launch(int T, int E, int k, const float *logits, const int32_t *ids, const float *weights, const float *dweights,
                             bool renorm, float *dlogits, hipStream_t st)
 {
-    auto *f = E <= 64 ? route_bwd<1> : E <= 128 ? route_bwd<2> : E <= 256 ? route_bwd<4> : E <= 512 ? route_bwd<8> : route_bwd<16>;
+    auto *f = E <= 16    ? route_bwd<16, 1>
+              : E <= 32  ? route_bwd<16, 2>
+              : E <= 64  ? route_bwd<16, 4>
+              : E <= 128 ? route_bwd<16, 8>
+              : E <= 256 ? route_bwd<16, 16>
+              : E <= 512 ? route_bwd<64, 8>
+                         : route_bwd<64, 16>;
     return f(T, E, k, logits, ids, weights, dweights, renorm, dlogits, st);
 }
 
