@@ -42,7 +42,7 @@ template <bool WHOLE>
 __device__ __forceinline__ lanes_u32x4 few_row(const uint16_t *row, int k, int K)
 {
     if constexpr (WHOLE) return load_unit8(row + k);
-    return k < K ? load_unit8(row + k, K - k) : lanes_u32x4{0u, 0u, 0u, 0u};
+    return k < K ? load_unit8(row + k, K - k, K) : lanes_u32x4{0u, 0u, 0u, 0u};
 }
 
 // Weights<>: what a wave holds of a step of kStep inputs of 16 outputs, kOps instructions' worth.

@@ -2,7 +2,7 @@
 // the group's weights, and the gradients of the rows and of the weights.
 //
 // One kernel in three forms.  A workgroup owns a tile BM x BN of one group's result and walks the reduction in stages of 64,
-// two of them in LDS; a wave keeps a tile WM x WN in registers as 16x16 results of v_mfma_f32_16x16x32_bf16.
+// two or four of them in LDS; a wave keeps a tile WM x WN in registers as 16x16 results of v_mfma_f32_16x16x32_bf16.
 // An operand lies in LDS as it lies in memory, in units of eight values (16 bytes):
 //   * reduction innermost (both operands of the forward product, the rows of the gradient of the rows): [row][64]; a lane
 //     reads the eight values of its row that one instruction takes.  The unit c of a row is stored in place c ^ (row & 7), so
@@ -31,7 +31,6 @@ typedef int gg_i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t gg_u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStage = 64;                          // reduction of a stage: two matrix instructions' of 32
-constexpr int kBuffers = 2;                         // stages in LDS
 constexpr int kIndices = 4096;                      // row indices of the reduction kept in LDS at a time
 constexpr uint32_t kFarOffset = 0xfffffff0u;        // out of range of every descriptor here
 constexpr uint64_t kFarRecords = 0xffffffe0ull;     // so that no sum of an offset in range and a load's width reaches 2^32
@@ -113,6 +112,7 @@ struct Operand {
     const char *base;                 // of the tile; GATHER: of the tensor (RED_OUTER: of the tile's columns in it)
     int64_t ld, bytes;                // from row to row; from base to the end of what may be read
     int red, count;                   // length of the reduction; rows or columns of the tile that exist
+    int length;                       // RED_OUTER: of a row in memory, columns of other tiles included
     const int32_t *rows;              // GATHER: of the tile's rows (innermost), of the reduction's (outermost)
     int src_rows;
     const int *index;                 // kIndexed: in LDS, entry k % kIndices is row k's, -1: none
@@ -197,10 +197,10 @@ struct Operand {
             held[i] = lanes_u32x4{0u, 0u, 0u, 0u};
             const int u = unit_of(tid, i) * 8;
             if constexpr (!RED_OUTER) {
-                if (at[i] && k0 + u < red) held[i] = load_unit8(reinterpret_cast<const uint16_t *>(at[i]) + k0 + u, red - k0 - u);
+                if (at[i] && k0 + u < red) held[i] = load_unit8(reinterpret_cast<const uint16_t *>(at[i]) + k0 + u, red - k0 - u, red);
             } else {
                 const int k = k0 + lds_row(tid, i), from = k < red && u < count ? (kIndexed ? src[i] : k) : -1;
-                if (from >= 0) held[i] = load_unit8(reinterpret_cast<const uint16_t *>(base + from * ld) + u, count - u);
+                if (from >= 0) held[i] = load_unit8(reinterpret_cast<const uint16_t *>(base + from * ld) + u, count - u, length);
             }
         }
     }
@@ -240,8 +240,9 @@ __device__ __forceinline__ void gg_wait()
 // four floats at any of their addresses
 struct __attribute__((packed, aligned(4))) Floats4 { gg_f32x4 v; };
 
-template <int FORM, int BM, int BN, int WM, int WN, bool DMA, bool GATHER, bool OUT_F32>
+template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA, bool GATHER, bool OUT_F32>
 struct GroupedTile {
+    static constexpr int kBuffers = BUFFERS;                                 // stages in LDS
     static constexpr int kThreads = (BM / WM) * (BN / WN) * 64;
     using A = Operand<BM, kThreads, FORM == GROUPED_DW, DMA, GATHER && FORM == GROUPED_FWD>;
     using B = Operand<BN, kThreads, FORM != GROUPED_FWD, DMA, GATHER && FORM == GROUPED_DW>;
@@ -271,6 +272,8 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
     B.ld = p.ldb;
     A.src_rows = B.src_rows = p.src_rows;
     A.rows = B.rows = nullptr;
+    A.length = p.out_rows;
+    B.length = p.cols;
     GroupTiles tiles;
     if constexpr (FORM != GROUPED_DW) tiles.init(p.offsets, p.E, p.M, BM, p.col_tiles);
 
@@ -323,13 +326,14 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         }
     };
     // Half a stage is in registers while the matrix cores work on the other half.  In the second half of stage s the first half of
-    // s+1 is read and stage s+2 asked for, into the buffer that s has left: every wave has its last values in registers.  It is waited
-    // for a stage later.  Stages of 32 in four buffers, three under way, were slower where the reduction is
-    // innermost, for the memory then gives half a cache line a row (16384 x 2048 x 4160 forward: 1074 against 1160 TFLOP/s).
+    // s+1 is read, and a stage asked for into the buffer that s has left: every wave has its last values in registers.  It is waited
+    // for kBuffers - 1 stages later.  (Stages of 32 in four buffers were slower where the reduction is innermost, for the memory
+    // then gives half a cache line a row: 16384 x 2048 x 4160 forward 1074 against 1160 TFLOP/s.)
     constexpr int kLoads = T::A::kUnits + T::B::kUnits;
-    int *const index = reinterpret_cast<int *>(grouped_lds + kBuffers * T::kStageBytes);
-    const auto buffer = [&](int s) { return grouped_lds + (s & 1) * T::kStageBytes; };
-    static_assert(kBuffers == 2, "the halves of a stage below");
+    int *const index = reinterpret_cast<int *>(grouped_lds + T::kBuffers * T::kStageBytes);
+    constexpr int kBuffers = T::kBuffers;
+    const auto buffer = [&](int s) { return grouped_lds + s % kBuffers * T::kStageBytes; };
+    static_assert(kBuffers == 2 || kBuffers == 4, "buffer()");
     const auto load = [&](int s, int i) {
         if (i < T::A::kUnits) A.unit(s, i, buffer(s), tid);
         else B.unit(s, i - T::A::kUnits, buffer(s) + T::A::kBytes, tid);
@@ -364,7 +368,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         constexpr bool kSecond = decltype(half)::value;
         if constexpr (kSecond) {
             commit(s + 1);
-            land(std::integral_constant<int, 0>{});          // stage s+1; and this wave has what it read of stage s
+            land(std::integral_constant<int, kBuffers - 2>{});      // stage s+1; and this wave has what it read of stage s
             if (T::B::kIndexed && (s + kBuffers) % (kIndices / kStage) == 0) {     // the next indices, rarely
                 B.load_indices(index, (s + kBuffers) * kStage, tid);
                 __syncthreads();
@@ -396,7 +400,8 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
     // (dX of 16384 x 4096 x 2048 with ReLU: 476 us).
     constexpr int kUnit = OUT_F32 ? 4 : 8, kAcrossUnits = WN / kUnit;                   // values and units of a row
     constexpr int kRoom = T::kOutBytes / (T::kThreads / 64) / (kAcrossUnits * 16), kRows = kRoom < WM ? kRoom : WM;
-    static_assert(kRows % 16 == 0 && WM % kRows == 0 && (kAcrossUnits & 7) == 0 && 64 % kAcrossUnits == 0, "whole tiles and rows");
+    static_assert(kRows % 16 == 0 && WM % kRows == 0 && (kAcrossUnits & 3) == 0 && 64 % kAcrossUnits == 0, "whole tiles and rows");
+    constexpr int kTwist = kAcrossUnits < 8 ? 3 : 7;                                    // neighbouring rows fall on other banks
     char *const mine = grouped_lds + T::kOutAt + wave * (kRows * kAcrossUnits * 16);
     const auto leave = [&](const GroupedOut &out) {
         // the compiler may not know that the lane is the same for every tile: it would keep all the addresses below in registers
@@ -419,7 +424,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
                         }
                     }
                     const int r = i * 16 + (lane & 15), n = j * 16 + (lane >> 4) * 4;
-                    char *at = mine + (r * kAcrossUnits + ((n / kUnit) ^ (r & 7))) * 16;
+                    char *at = mine + (r * kAcrossUnits + ((n / kUnit) ^ (r & kTwist))) * 16;
                     if constexpr (OUT_F32) *reinterpret_cast<gg_f32x4 *>(at) = v;
                     else *reinterpret_cast<gg_u32x2 *>(at + (n & 4) * 2) = gg_u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
                 }
@@ -427,13 +432,13 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             for (int i = 0; i < kRows * kAcrossUnits / 64; ++i) {
                 const int r = i * (64 / kAcrossUnits) + lane / kAcrossUnits, u = lane % kAcrossUnits;
                 const int row = wm + r0 + r, n = wn + u * kUnit, left = out.cols - n;
-                lanes_u32x4 v = *reinterpret_cast<const lanes_u32x4 *>(mine + (r * kAcrossUnits + (u ^ (r & 7))) * 16);
+                lanes_u32x4 v = *reinterpret_cast<const lanes_u32x4 *>(mine + (r * kAcrossUnits + (u ^ (r & kTwist))) * 16);
                 if (row >= out.rows || left <= 0) continue;
                 const int64_t at = out.c0 + (int64_t)row * p.ldc + n;
                 if constexpr (FORM == GROUPED_DX) {
                     if (p.act != POLYDL_ACT_NONE) {
                         const uint16_t *h = p.h + out.h0 + (int64_t)row * p.ldh + n;
-                        const lanes_u32x4 x = kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit)) : load_unit4(h);
+                        const lanes_u32x4 x = kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit), p.cols) : load_unit4(h);
 #pragma unroll
                         for (int q = 0; q < kUnit; ++q) {
                             const float y = q & 1 ? bf16_hi(x[q >> 1]) : bf16_lo(x[q >> 1]);
@@ -533,10 +538,10 @@ static hipError_t ask_lds(int bytes)
     return e;
 }
 
-template <int FORM, int BM, int BN, int WM, int WN, bool DMA, bool GATHER, bool OUT_F32>
+template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA, bool GATHER, bool OUT_F32>
 static hipError_t grouped_run(const GroupedProblem &q, hipStream_t st)
 {
-    using T = GroupedTile<FORM, BM, BN, WM, WN, DMA, GATHER, OUT_F32>;
+    using T = GroupedTile<FORM, BM, BN, WM, WN, BUFFERS, DMA, GATHER, OUT_F32>;
     constexpr auto kernel = grouped_kernel<T, FORM, BM, BN, WM, WN, OUT_F32>;
     GroupedArgs a{q.E, q.M, q.out_rows, q.cols, q.red, q.offsets, q.rows, q.src_rows, reinterpret_cast<const char *>(q.a),
                   reinterpret_cast<const char *>(q.b), q.lda * 2, q.ldb * 2, q.c, q.ldc, q.accumulate, q.act, q.h, q.ldh, 0, 0};
@@ -562,15 +567,15 @@ static hipError_t grouped_run(const GroupedProblem &q, hipStream_t st)
     return launch_kernel(kernel, dim3((unsigned)tiles), dim3(T::kThreads), T::kLds, st, a);
 }
 
-template <int FORM, int BM, int BN, int WM, int WN, bool DMA>
+template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA>
 static hipError_t grouped_pick_types(const GroupedProblem &q, hipStream_t st)
 {
     if constexpr (FORM == GROUPED_DX)
-        return q.out_f32 ? grouped_run<FORM, BM, BN, WM, WN, DMA, false, true>(q, st) : grouped_run<FORM, BM, BN, WM, WN, DMA, false, false>(q, st);
+        return q.out_f32 ? grouped_run<FORM, BM, BN, WM, WN, BUFFERS, DMA, false, true>(q, st) : grouped_run<FORM, BM, BN, WM, WN, BUFFERS, DMA, false, false>(q, st);
     else if (q.rows)
-        return q.out_f32 ? grouped_run<FORM, BM, BN, WM, WN, DMA, true, true>(q, st) : grouped_run<FORM, BM, BN, WM, WN, DMA, true, false>(q, st);
+        return q.out_f32 ? grouped_run<FORM, BM, BN, WM, WN, BUFFERS, DMA, true, true>(q, st) : grouped_run<FORM, BM, BN, WM, WN, BUFFERS, DMA, true, false>(q, st);
     else
-        return q.out_f32 ? grouped_run<FORM, BM, BN, WM, WN, DMA, false, true>(q, st) : grouped_run<FORM, BM, BN, WM, WN, DMA, false, false>(q, st);
+        return q.out_f32 ? grouped_run<FORM, BM, BN, WM, WN, BUFFERS, DMA, false, true>(q, st) : grouped_run<FORM, BM, BN, WM, WN, BUFFERS, DMA, false, false>(q, st);
 }
 
 // Whether both operands can go into LDS in whole units at 32-bit offsets: 16-byte rows, and offsets inside a tile (rows by
@@ -586,32 +591,39 @@ static bool grouped_whole_units(const GroupedProblem &q, int bm, int bn)
     return q.out_rows % 8 == 0 && kStage * q.lda * 2 < last && (q.rows ? (int64_t)q.src_rows : (int64_t)kStage) * q.ldb * 2 < last;
 }
 
-// Tiles of 256 x 256, one workgroup on a compute unit, or of 128 x 128, two: what is left of the last round decides.  A round of
-// the small ones takes 0.65 of a round of the large ones and does half the work (4096 x 4096 x 4096: 117 us in one round of 256, 155 in two of
-// 128).  Tiles are counted for groups of the mean length, each with half a tile more.  Measured both ways, forward, us for 256 / 128: 16 groups of 256
-// rows, 2048 x 2048, 66 / 80; of 400, 99 / 95; of 1024, 176 / 200; one of 4096, 57 / 42.  Up to 128 rows a group the large tiles
-// are mostly empty (16 groups of 128: 62 / 52).  Weight gradients of few tiles a group need the small ones to even the groups out (64 groups of 512 rows, 512 x
-// 512: 74 / 55; 8 of 1024 rows, 1024 x 2048: 51 / 56).
+// Rounds of `at_a_time` workgroups that tiles of `tile` squared take, groups of the mean length taken to end in half a tile each.
 template <int FORM>
-static bool grouped_large_tiles(const GroupedProblem &q)
+static int64_t grouped_rounds(const GroupedProblem &q, int64_t tile, int64_t at_a_time)
 {
-    const int64_t cus = compute_units();
-    const auto rounds = [&](int64_t tile, int64_t at_a_time) {
-        const int64_t across = (q.cols + tile - 1) / tile;
-        const int64_t down = FORM == GROUPED_DW ? (q.out_rows + tile - 1) / tile * q.E
-                             : q.E == 1         ? (q.M + tile - 1) / tile
-                                                : (q.M + q.E * (tile / 2)) / tile;
-        return (across * down + at_a_time - 1) / at_a_time;
-    };
-    if (FORM == GROUPED_DW ? ((int64_t)q.out_rows + 255) / 256 * ((q.cols + 255) / 256) < 8 : q.M <= 128 * (int64_t)q.E) return false;
-    return (double)rounds(256, cus) <= 0.65 * (double)rounds(128, 2 * cus);
+    const int64_t across = (q.cols + tile - 1) / tile;
+    const int64_t down = FORM == GROUPED_DW ? (q.out_rows + tile - 1) / tile * q.E
+                         : q.E == 1         ? (q.M + tile - 1) / tile
+                                            : (q.M + q.E * (tile / 2) + tile - 1) / tile;
+    return (across * down + at_a_time - 1) / at_a_time;
 }
 
+// Tiles of 256 (one workgroup on a compute unit), of 128 (two) or of 64 (two, with four stages in LDS; operands that go through registers: three,
+// with two).  What is left of the last round decides: a round of 128 takes 0.65 of a round of 256 and does half the work (4096 x 4096 x
+// 4096: 117 us in one round of 256, 155 in two of 128); one of 64 takes half a round of 128, for a quarter of the work, and where 64 fits one
+// round it is the stages' latency that counts, of which it has more under way.  Measured both ways, forward, us:
+//   256 / 128: 16 groups of 256 rows, 2048 x 2048, 66 / 80; of 400, 99 / 95; of 1024, 176 / 200; one of 4096, 57 / 42;
+//   64 / 128: one group of 1024 rows, 1024 x 1024, 11 / 18; 32 of 64, 512 x 512, 10 / 13; 16 of 256, 1024 x 1024, 30 / 23;
+//   through registers, 64 / 128: 7 of 143 rows, 777 x 531, 13 / 20; 8 of 256, 1001 x 777, 21 / 27; 8 of 2048, 2047 x 2047, 424 / 305.
+// Up to 128 rows a group tiles of 256 are mostly empty (16 groups of 128: 62 / 52).  Weight gradients of few tiles a group need smaller ones
+// to even the groups out (64 groups of 512 rows, 512 x 512: 74 / 55; 8 of 1024 rows, 1024 x 2048: 51 / 56).
 template <int FORM>
 static hipError_t grouped_pick(const GroupedProblem &q, hipStream_t st)
 {
-    if (!grouped_whole_units(q, 256, 256)) return grouped_pick_types<FORM, 128, 128, 64, 64, false>(q, st);
-    return grouped_large_tiles<FORM>(q) ? grouped_pick_types<FORM, 256, 256, 128, 64, true>(q, st) : grouped_pick_types<FORM, 128, 128, 64, 64, true>(q, st);
+    const int64_t cus = compute_units();
+    const double of128 = (double)grouped_rounds<FORM>(q, 128, 2 * cus);
+    if (!grouped_whole_units(q, 256, 256)) {
+        if (0.5 * (double)grouped_rounds<FORM>(q, 64, 3 * cus) <= of128) return grouped_pick_types<FORM, 64, 64, 32, 32, 2, false>(q, st);
+        return grouped_pick_types<FORM, 128, 128, 64, 64, 2, false>(q, st);
+    }
+    const bool empty = FORM == GROUPED_DW ? ((int64_t)q.out_rows + 255) / 256 * ((q.cols + 255) / 256) < 8 : q.M <= 128 * (int64_t)q.E;
+    if (!empty && (double)grouped_rounds<FORM>(q, 256, cus) <= 0.65 * of128) return grouped_pick_types<FORM, 256, 256, 128, 64, 2, true>(q, st);
+    if (0.55 * (double)grouped_rounds<FORM>(q, 64, 2 * cus) <= of128) return grouped_pick_types<FORM, 64, 64, 32, 32, 4, true>(q, st);
+    return grouped_pick_types<FORM, 128, 128, 64, 64, 2, true>(q, st);
 }
 
 hipError_t grouped_gemm_launch(const GroupedProblem &q, hipStream_t st)

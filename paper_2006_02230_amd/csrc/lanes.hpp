@@ -92,15 +92,26 @@ __device__ __forceinline__ lanes_u32x4 load_unit4(const uint16_t *p)
     const Unit4 u = *reinterpret_cast<const Unit4 *>(p);
     return lanes_u32x4{u.v[0], u.v[1], 0u, 0u};
 }
-// the first n of them (0 <= n <= 8), zeros for the rest; nothing past them is read
-__device__ __forceinline__ lanes_u32x4 load_unit8(const uint16_t *p, int n)
+// The first n of them, zeros for the rest, in a row of `length` that ends n values from p on (n >= 1; more than 8: as 8).  Nothing outside
+// the row is read: where n < 8 the row's last eight values are loaded and shifted.  (One by one they cost a load's latency each, for the whole
+// wave.)  A wave without such a lane does not wait for the load here.
+__device__ __forceinline__ lanes_u32x4 load_unit8(const uint16_t *p, int n, int length)
 {
     if (n >= 8) return load_unit8(p);
     lanes_u32x4 v = {0u, 0u, 0u, 0u};
+    if (length < 8) {
 #pragma unroll
-    for (int i = 0; i < 7; ++i)
-        if (i < n) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
-    return v;
+        for (int i = 0; i < 7; ++i)
+            if (i < n) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+        return v;
+    }
+    const int past = 8 - n;
+    v = load_unit8(p - past);
+    v = past & 4 ? lanes_u32x4{v[2], v[3], 0u, 0u} : v;
+    v = past & 2 ? lanes_u32x4{v[1], v[2], v[3], 0u} : v;
+    return past & 1 ? lanes_u32x4{__builtin_amdgcn_alignbit(v[1], v[0], 16u), __builtin_amdgcn_alignbit(v[2], v[1], 16u),
+                                  __builtin_amdgcn_alignbit(v[3], v[2], 16u), v[3] >> 16}
+                    : v;
 }
 __device__ __forceinline__ void store_unit8(uint16_t *p, lanes_u32x4 v, int n)
 {

@@ -415,7 +415,7 @@ __global__ __launch_bounds__(256) void combine_kernel(int T, int k, int M, int D
             const bool there = (unsigned)s < (unsigned)M;
             w[j] = !there ? 0.f : weights ? weights[t * k + j0 + j] : 1.f;
             v[j] = lanes_u32x4{0u, 0u, 0u, 0u};
-            if (there) v[j] = load_unit8(y + (size_t)s * D + col, n);
+            if (there) v[j] = load_unit8(y + (size_t)s * D + col, n, D);
         }
 #pragma unroll
         for (int j = 0; j < 4; ++j)
@@ -474,9 +474,9 @@ __global__ __launch_bounds__(256) void combine_bwd_kernel(int64_t MT, int k, int
 #pragma unroll 2
     for (int col = lane * 8; col < D; col += 512) {
         const int n = min(8, D - col);
-        const lanes_u32x4 dv = load_unit8(d + col, n);
+        const lanes_u32x4 dv = load_unit8(d + col, n, D);
         lanes_u32x4 yv = {0u, 0u, 0u, 0u}, ov;
-        if (dweights) yv = load_unit8(yr + col, n);
+        if (dweights) yv = load_unit8(yr + col, n, D);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
             const float lo = bf16_lo(dv[q]), hi = bf16_hi(dv[q]);

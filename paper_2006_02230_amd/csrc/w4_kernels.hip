@@ -24,7 +24,7 @@ __global__ __launch_bounds__(64) void w4_pack_kernel(int N, int K, int group, in
     for (int i = 0; i < 4; ++i) {
         const int k = s * 128 + i * 32 + quad * 8;
         lanes_u32x4 u = {0u, 0u, 0u, 0u};
-        if (n < N && k < K) u = load_unit8(w + (e * N + n) * K + k, K - k);
+        if (n < N && k < K) u = load_unit8(w + (e * N + n) * K + k, K - k, K);
         lo[i] = hi[i] = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
