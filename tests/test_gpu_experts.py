@@ -366,6 +366,22 @@ def test_grouped_gradients_against_differences(P):
     assert f(x, w + sw) - f(x, w) == (dw.double() * sw.double()).sum()
 
 
+@pytest.mark.parametrize("N,K,how", [(72, 64, "dense"), (75, 61, "dense"), (136, 520, "strided"), (4096, 4096, "dense")])
+def test_gradient_of_weights_over_long_groups(P, N, K, how):
+    # more rows by index than are held at a time (4096), in every kind of tile
+    import torch
+    counts = (4096, 9001, 3) if N < 4096 else (9001,)
+    offsets, M = ragged(counts, 2)
+    g = gen(N)
+    dy, x = randn(g, M, N).bfloat16(), randn(g, 5000, K).bfloat16()
+    rows = rows_for(M, 5000, offsets, 4)
+    got = P.grouped_gemm_dw_bf16(views(dy, how), views(x, how), ints(offsets), rows=ints(rows))
+    xs = reference_rows(x, rows)
+    for e in range(len(counts)):
+        a, b = offsets[e], offsets[e + 1]
+        close(got[e], dy[a:b].double().T @ xs[a:b], dy[a:b].double().abs().T @ xs[a:b].abs(), counts[e], e)
+
+
 def test_grouped_infinities_stay_in_their_rows(P):
     import torch
     offsets, M = ragged((70, 60), 0)
@@ -525,6 +541,41 @@ def test_w4_strided_result_and_offsets_past_32_bits(P):
     P.w4_gemm_bf16(x, q, scales, N, 128, offsets=offsets, out=out[:, :N])
     alone = P.w4_gemm_bf16(x[1:], one.q, one.scales, N, 128)
     assert torch.equal(out[1:, :N], alone) and bool((out[:, N:] == -1).all()) and bool((out[0, :N] == 0).all())
+
+
+# ---- the layer --------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("T,D,F,E,k", [(1, 64, 128, 4, 2), (100, 72, 88, 6, 3), (700, 256, 512, 8, 2)])
+def test_layer_against_64_bits(P, T, D, F, E, k):
+    import torch
+    from paper_2006_02230_amd.expert_layer import ExpertLayer
+    g = gen(T)
+    router = randn(g, D, E) * D ** -0.5
+    w1, w2 = (randn(g, E, F, D) * D ** -0.5).bfloat16(), (randn(g, E, D, F) * F ** -0.5).bfloat16()
+    x, dout = randn(g, T, D).bfloat16(), randn(g, T, D).bfloat16()
+    layer = ExpertLayer(router, w1, w2, k)
+    out = layer.forward(x)
+    grads = layer.backward(dout)
+    ids = layer.kept[3].ids.long()
+    X, R, W1, W2 = (v.double().requires_grad_() for v in (x, router, w1, w2))
+    p = torch.gather(X @ R, 1, ids).softmax(1)
+    want = torch.zeros(T, D, dtype=torch.float64, device="cuda")
+    for e in range(E):
+        there = (ids == e)
+        t = there.any(1).nonzero()[:, 0]
+        want = want.index_add(0, t, (p * there).sum(1)[t, None] * (torch.relu(X[t] @ W1[e].T) @ W2[e].T))
+    want.backward(dout.double())
+    # three roundings to bfloat16 on the way of every term forward and four backward, each of 2^-8 of it, independent: 2^-8 sqrt(n) of the norm
+    # and a half more for the terms' unequal sizes
+    for got, ref, n in ((out, want, 3), (grads.x, X.grad, 4), (grads.router, R.grad, 4), (grads.w1, W1.grad, 4), (grads.w2, W2.grad, 4)):
+        off = (got.double() - ref).norm() / ref.norm()
+        assert off <= 1.5 * n ** 0.5 * 2.0 ** -8, (float(off), n)
+
+
+def test_layer_trains_and_answers_in_4_bits(P):
+    from paper_2006_02230_amd.expert_layer import main
+    first, last, coded = main()
+    assert last < 0.5 * first and coded < first, (first, last, coded)
 
 
 # ---- streams and graphs ------------------------------------------------------------------------------------------------
