@@ -61,12 +61,12 @@ struct GroupTiles {
             if (past) {
                 const int l = __builtin_ctzll(past), high = lane_of(tiles, l);
                 const int at = id - before - (lane_of(upto, l) - high * col_tiles);
-                const int band = at / max(high * 4, 1), n0 = band * 4, width = max(min(4, col_tiles - n0), 1), in = at - band * high * 4;
-                t->e = e0 + l;
+                const int band = wave_value(at / max(high * 4, 1)), n0 = band * 4, width = max(min(4, col_tiles - n0), 1), in = at - band * high * 4;
+                t->e = wave_value(e0 + l);
                 t->lo = lane_of(g.lo, l);
                 t->hi = lane_of(g.hi, l);
-                t->m = in / width;
-                t->n = n0 + in - t->m * width;
+                t->m = wave_value(in / width);
+                t->n = wave_value(n0 + in - t->m * width);
                 // offsets that are none (groups that overlap many times) may make the sums above wrap around
                 return (unsigned)t->m < (unsigned)high && (unsigned)t->n < (unsigned)col_tiles;
             }

@@ -49,11 +49,13 @@ struct GroupedArgs {
     int row_tiles, col_tiles;      // of one C_e (GROUPED_DW); columns (others)
 };
 
-// A raw buffer descriptor of `bytes` bytes from base (none if negative).
-__device__ __forceinline__ gg_i32x4 gg_rsrc(const char *base, int64_t bytes)
+// A raw buffer descriptor of `bytes` bytes from base (none if negative), in operations of 32 bits: there are no scalar comparisons of 64.
+__device__ __forceinline__ gg_i32x4 gg_rsrc(uint64_t base, int64_t bytes)
 {
-    const uint64_t n = bytes < 0 ? 0 : (uint64_t)bytes > kFarRecords ? kFarRecords : (uint64_t)bytes, at = (uint64_t)base;
-    return gg_i32x4{(int)(uint32_t)at, (int)((uint32_t)(at >> 32) & 0xffffu), (int)(uint32_t)n, 0x00020000};
+    const int high = (int)(bytes >> 32);
+    const uint32_t low = (uint32_t)bytes, most = (uint32_t)kFarRecords;
+    const uint32_t n = high < 0 ? 0u : high > 0 ? most : low < most ? low : most;
+    return gg_i32x4{(int)(uint32_t)base, (int)((uint32_t)(base >> 32) & 0xffffu), (int)n, 0x00020000};
 }
 // Sixteen bytes a lane into LDS at `lds` + 16 * lane; not waited for.  As assembly, because the compiler puts a wait for every such
 // load before each transposing LDS read, whichever buffer it reads (measured with stages of 32 at 16384 x 4096 x 2048: dX 1112
@@ -120,7 +122,13 @@ struct Operand {
     int32_t src[kIndexed ? kUnits : 1];                          // rows of the stage to be fetched
     const char *at[!DMA && !RED_OUTER ? kUnits : 1];             // of the unit's row, NULL: none
     lanes_u32x4 held[DMA ? 1 : kUnits];
-    gg_i32x4 rsrc;                    // of the stage to be fetched
+    uint32_t wave_at;                 // DMA: where the wave's units lie in a stage
+    // DMA: the descriptor of the stage to be fetched, kept from stage to stage: its base, what it may read from there on, and how far both
+    // move a stage.  Reduction innermost and rows by index: lanes out of range are known by their offsets alone, and it may read on.
+    uint64_t at_base;
+    int64_t may_read;
+    uint32_t stage_bytes;
+    gg_i32x4 rsrc;
 
     // the permutation: of the blocks of 16 columns in reduction row kr, of the units of row r
     static __device__ __forceinline__ int spread(int kr)
@@ -139,6 +147,10 @@ struct Operand {
 
     __device__ __forceinline__ void init(int tid)
     {
+        wave_at = (uint32_t)__builtin_amdgcn_readfirstlane(tid >> 6) * 1024u;
+        at_base = wave_value((uint64_t)base);
+        may_read = RED_OUTER && !GATHER ? (int64_t)wave_value((uint64_t)bytes) : (int64_t)kFarRecords;
+        stage_bytes = !RED_OUTER ? kStage * 2 : GATHER ? 0u : (uint32_t)wave_value((int)((uint32_t)ld * kStage));
 #pragma unroll
         for (int i = 0; i < kUnits; ++i) {
             const int r = lds_row(tid, i), u = unit_of(tid, i);
@@ -164,13 +176,22 @@ struct Operand {
         }
     }
 
-    // A stage is fetched in three steps: begin() once, unit() for each unit, commit() when registers held it.
+    // A stage is fetched in three steps: begin() once, unit() for each unit, commit() when registers held it; stage after stage.
     __device__ __forceinline__ void begin(int s, int tid)
     {
         const int k0 = s * kStage;
         if constexpr (DMA) {
-            const int64_t skip = RED_OUTER ? (GATHER ? 0 : (int64_t)k0 * ld) : (int64_t)k0 * 2;
-            rsrc = gg_rsrc(base + skip, bytes - skip);
+            rsrc = gg_rsrc(at_base, may_read);
+            at_base += stage_bytes;
+            if (RED_OUTER && !GATHER) may_read -= (int64_t)stage_bytes;
+            if constexpr (!RED_OUTER) {
+                // the reduction's end, and stages past it: from here on these lanes have nothing to load
+                if (k0 + kStage > red) {
+#pragma unroll
+                    for (int i = 0; i < kUnits; ++i)
+                        if (k0 + unit_of(tid, i) * 8 >= red) off[i] = kFarOffset;
+                }
+            }
         }
         if constexpr (kIndexed) {
 #pragma unroll
@@ -185,14 +206,9 @@ struct Operand {
         if (!mine(tid)) return;
         const int k0 = s * kStage;
         if constexpr (DMA) {
-            const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
             uint32_t o = off[i];
-            if constexpr (!RED_OUTER) {
-                if (k0 + unit_of(tid, i) * 8 >= red) o = kFarOffset;
-            } else if constexpr (GATHER) {
-                o = src[i] < 0 || o == kFarOffset ? kFarOffset : (uint32_t)src[i] * (uint32_t)ld + o;
-            }
-            gg_dma(rsrc, gg_lds_offset(lds) + (uint32_t)(i * THREADS + wave * 64) * 16u, o);
+            if constexpr (kIndexed) o = src[i] < 0 || o == kFarOffset ? kFarOffset : (uint32_t)src[i] * (uint32_t)ld + o;
+            gg_dma(rsrc, gg_lds_offset(lds) + wave_at + (uint32_t)(i * THREADS) * 16u, o);
         } else {
             held[i] = lanes_u32x4{0u, 0u, 0u, 0u};
             const int u = unit_of(tid, i) * 8;
@@ -213,16 +229,17 @@ struct Operand {
         }
     }
 
-    // What one instruction takes of rows r0 .. r0+15.
-    static __device__ __forceinline__ lanes_u32x4 operand(const char *lds, int r0, int kk, int lane)
+    // What one instruction takes of rows r0 + 16 i .. r0 + 16 i + 15, half kk of the stage; r0 a multiple of 64.  Only i and kk are known to the
+    // compiler, so what they add is kept out of the lane's part: it goes into the instruction.
+    static __device__ __forceinline__ lanes_u32x4 operand(const char *lds, int r0, int i, int kk, int lane)
     {
         if constexpr (!RED_OUTER) {
-            const int r = r0 + (lane & 15);
-            return *reinterpret_cast<const lanes_u32x4 *>(lds + r * (kStage * 2) + (((kk * 4 + (lane >> 4)) ^ turn(lane & 15)) * 16));
+            const char *at = lds + (r0 + (lane & 15)) * (kStage * 2) + (((lane >> 4) ^ turn(lane & 15)) * 16 ^ kk * 64);
+            return *reinterpret_cast<const lanes_u32x4 *>(at + i * (16 * kStage * 2));
         } else {
-            const int kr = kk * 32 + (lane >> 4) * 8 + ((lane & 15) >> 2);
-            const char *at = lds + kr * (R * 2) + ((r0 >> 4) ^ spread(kr)) * 32 + (lane & 3) * 8;
-            const gg_u32x2 lo = gg_read_tr(at), hi = gg_read_tr(at + 4 * R * 2);   // spread(kr + 4) == spread(kr) here
+            const int kr = (lane >> 4) * 8 + ((lane & 15) >> 2);
+            const char *at = lds + kr * (R * 2) + ((r0 >> 4) + i ^ spread(kr)) * 32 + (lane & 3) * 8 + kk * (32 * R * 2);
+            const gg_u32x2 lo = gg_read_tr(at), hi = gg_read_tr(at + 4 * R * 2);   // spread(kr + 4) == spread(kr + 32) == spread(kr) here
             return lanes_u32x4{lo[0], lo[1], hi[0], hi[1]};
         }
     }
@@ -304,11 +321,13 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             return t.e < p.E ? (p.red + kStage - 1) / kStage : 0;   // slots behind the last group: a result of zeros
         } else {
             // groups differ in length, so every die takes an eighth of each one's tiles, another eighth from group to group
-            const int per = p.row_tiles * p.col_tiles, eighth = (per + 7) >> 3, at = id >> 3, e = at / eighth;
+            const int per = p.row_tiles * p.col_tiles, eighth = (per + 7) >> 3, at = id >> 3, e = wave_value(at / eighth);
             const int in = ((id + e) & 7) * eighth + at - e * eighth;
             if (in >= per) return -1;
-            const int m = in / p.col_tiles, n = in - m * p.col_tiles;
-            const GroupRows g = group_rows(p.offsets, e, p.E, p.M);
+            const int m = wave_value(in / p.col_tiles), n = in - m * p.col_tiles;
+            GroupRows g = group_rows(p.offsets, e, p.E, p.M);
+            g.lo = wave_value(g.lo);
+            g.hi = wave_value(g.hi);
             const int red = g.hi - g.lo;
             out.rows = min(BM, p.out_rows - m * BM);
             out.cols = min(BN, p.cols - n * BN);
@@ -359,8 +378,8 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
     };
     // the n-th operand of a stage: the columns', then the rows'
     const auto read = [&](int s, int kk, int n, lanes_u32x4 (&a)[MI], lanes_u32x4 (&b)[NI]) {
-        if (n < NI) b[n] = T::B::operand(buffer(s) + T::A::kBytes, wn + n * 16, kk, lane);
-        else a[n - NI] = T::A::operand(buffer(s), wm + (n - NI) * 16, kk, lane);
+        if (n < NI) b[n] = T::B::operand(buffer(s) + T::A::kBytes, wn, n, kk, lane);
+        else a[n - NI] = T::A::operand(buffer(s), wm, n - NI, kk, lane);
     };
     gg_f32x4 acc[MI][NI];
     const auto step = [&](int s, auto half, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI],

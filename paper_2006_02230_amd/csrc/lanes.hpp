@@ -39,6 +39,13 @@ __device__ __forceinline__ int wave_prefix(int x)
 #undef STEP
     return x;
 }
+// A value that is the same for all lanes, into scalar registers: what a load or a division gives is in vector registers, and what is
+// computed from it would follow.
+__device__ __forceinline__ int wave_value(int x) { return __builtin_amdgcn_readfirstlane(x); }
+__device__ __forceinline__ uint64_t wave_value(uint64_t x)
+{
+    return (uint64_t)(uint32_t)wave_value((int)(uint32_t)(x >> 32)) << 32 | (uint32_t)wave_value((int)(uint32_t)x);
+}
 __device__ __forceinline__ int lane_of(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
 __device__ __forceinline__ float lane_of(float x, int lane)
 {
