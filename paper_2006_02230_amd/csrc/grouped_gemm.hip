@@ -275,11 +275,12 @@ struct GroupedTile {
 // What a finished tile leaves by: its rows and columns that exist, its first result, that of `h`.
 struct GroupedOut { int rows, cols; int64_t c0, h0; };
 
-template <class T, int FORM, int BM, int BN, int WM, int WN, bool OUT_F32>
+// PAST: results go past the L2 (a choice at run time, between the stores, costs dX of 32768 x 2048 by 512 6 us of 74)
+template <class T, int FORM, int BM, int BN, int WM, int WN, bool OUT_F32, bool PAST>
 __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
 {
     extern __shared__ __align__(1024) char grouped_lds[];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_value(tid >> 6);
     constexpr int kAcross = BN / WN, MI = WM / 16, NI = WN / 16;
     const int wm = wave / kAcross * WM, wn = wave % kAcross * WN;
 
@@ -382,9 +383,9 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         else a[n - NI] = T::A::operand(buffer(s), wm, n - NI, kk, lane);
     };
     gg_f32x4 acc[MI][NI];
-    const auto step = [&](int s, auto half, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI],
+    const auto step = [&](int s, auto half, auto busy, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI],
                           lanes_u32x4 (&b_next)[NI]) {
-        constexpr bool kSecond = decltype(half)::value;
+        constexpr bool kSecond = decltype(half)::value, kBusy = decltype(busy)::value;
         if constexpr (kSecond) {
             commit(s + 1);
             land(std::integral_constant<int, kBuffers - 2>{});      // stage s+1; and this wave has what it read of stage s
@@ -400,13 +401,14 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         for (int i = 0; i < MI; ++i) {
             // columns as the instruction's rows: a lane then holds four neighbouring columns of one row of the result
 #pragma unroll
-            for (int j = 0; j < NI; ++j) acc[i][j] = gg_mfma(b[j], a[i], acc[i][j]);
+            for (int j = 0; j < NI; ++j)
+                if constexpr (kBusy) acc[i][j] = gg_mfma(b[j], a[i], acc[i][j]);
             if (kSecond && i == 0) {
                 A.begin(s + kBuffers, tid);
                 B.begin(s + kBuffers, tid);
             }
 #pragma unroll
-            for (int n = i * kReads / kReadRows; n < (i + 1) * kReads / kReadRows && n < kReads; ++n) read(s + kSecond, !kSecond, n, a_next, b_next);
+            for (int n = i * kReads / kReadRows; n < (i + 1) * kReads / kReadRows && n < kReads && kBusy; ++n) read(s + kSecond, !kSecond, n, a_next, b_next);
             if constexpr (kSecond) {
 #pragma unroll
                 for (int l = i * kLoads / kLoadRows; l < (i + 1) * kLoads / kLoadRows && l < kLoads; ++l) load(s + kBuffers, l);
@@ -422,11 +424,39 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
     static_assert(kRows % 16 == 0 && WM % kRows == 0 && (kAcrossUnits & 3) == 0 && 64 % kAcrossUnits == 0, "whole tiles and rows");
     constexpr int kTwist = kAcrossUnits < 8 ? 3 : 7;                                    // neighbouring rows fall on other banks
     char *const mine = grouped_lds + T::kOutAt + wave * (kRows * kAcrossUnits * 16);
-    const auto leave = [&](const GroupedOut &out) {
+    // What the activation gave is asked for kAhead chunks of rows before it is needed, the first of them before the next tile's stages, where
+    // the wave's part of the tile is whole.  (Unit by unit as the results leave, every one of them waits for memory: dX of 16384 x 2048 x 4096 in 16
+    // uneven groups with ReLU 313 us -> 301; without the activation 269.)
+    constexpr int kChunks = WM / kRows, kPer = kRows * kAcrossUnits / 64, kWords = OUT_F32 ? 2 : 4;
+    constexpr int kAhead = FORM != GROUPED_DX ? 1 : 32 / (kPer * kWords) < kChunks ? 32 / (kPer * kWords) : kChunks;
+    // go_on() starts the next tile
+    const auto leave = [&](const GroupedOut &out, auto go_on) {
         // the compiler may not know that the lane is the same for every tile: it would keep all the addresses below in registers
         // through the products, and spill
         int lane = tid & 63;
         if constexpr (T::kLoops) asm volatile("" : "+v"(lane));
+        const bool early = FORM == GROUPED_DX && p.act != POLYDL_ACT_NONE && out.rows >= wm + WM && out.cols >= wn + WN && p.ldh < (1 << 24);
+        std::conditional_t<OUT_F32, gg_u32x2, lanes_u32x4> held_h[kAhead][kPer];
+        // one address a lane, the rest of it the same for the wave
+        const uint64_t h_base = wave_value((uint64_t)(p.h + out.h0 + (int64_t)wm * p.ldh + wn));
+        const uint32_t h_off = (uint32_t)(lane / kAcrossUnits) * (uint32_t)(p.ldh * 2) + (uint32_t)(lane % kAcrossUnits * kUnit) * 2u;
+        const auto ask_h = [&](int chunk) {
+            if (FORM != GROUPED_DX || !early || chunk >= kChunks) return;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                const uint64_t row = (uint64_t)(chunk * kRows + i * (64 / kAcrossUnits));
+                const uint16_t *at = reinterpret_cast<const uint16_t *>(h_base + row * 2 * (uint64_t)p.ldh + h_off);
+                if constexpr (OUT_F32) {
+                    const Unit4 u = *reinterpret_cast<const Unit4 *>(at);
+                    held_h[chunk % kAhead][i] = gg_u32x2{u.v[0], u.v[1]};
+                } else {
+                    held_h[chunk % kAhead][i] = load_unit8(at);
+                }
+            }
+        };
+#pragma unroll
+        for (int i = 0; i < kAhead; ++i) ask_h(i);
+        go_on();
 #pragma unroll
         for (int r0 = 0; r0 < WM; r0 += kRows) {
 #pragma unroll
@@ -456,8 +486,15 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
                 const int64_t at = out.c0 + (int64_t)row * p.ldc + n;
                 if constexpr (FORM == GROUPED_DX) {
                     if (p.act != POLYDL_ACT_NONE) {
-                        const uint16_t *h = p.h + out.h0 + (int64_t)row * p.ldh + n;
-                        const lanes_u32x4 x = kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit), p.cols) : load_unit4(h);
+                        lanes_u32x4 x;
+                        if (early) {
+                            const auto u = held_h[r0 / kRows % kAhead][i];
+                            if constexpr (OUT_F32) x = lanes_u32x4{u[0], u[1], 0u, 0u};
+                            else x = u;
+                        } else {
+                            const uint16_t *h = p.h + out.h0 + (int64_t)row * p.ldh + n;
+                            x = kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit), p.cols) : load_unit4(h);
+                        }
 #pragma unroll
                         for (int q = 0; q < kUnit; ++q) {
                             const float y = q & 1 ? bf16_hi(x[q >> 1]) : bf16_lo(x[q >> 1]);
@@ -472,16 +509,20 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
                     gg_f32x4 f = __builtin_bit_cast(gg_f32x4, v);
                     if (left >= 4) {
                         if (p.accumulate) f += reinterpret_cast<const Floats4 *>(c)->v;
-                        reinterpret_cast<Floats4 *>(c)->v = f;
+                        if constexpr (PAST) __builtin_nontemporal_store(f, &reinterpret_cast<Floats4 *>(c)->v);
+                        else reinterpret_cast<Floats4 *>(c)->v = f;
                     } else {
 #pragma unroll
                         for (int q = 0; q < 3; ++q)
                             if (q < left) c[q] = p.accumulate ? c[q] + f[q] : f[q];
                     }
                 } else {
-                    store_unit8(static_cast<uint16_t *>(p.c) + at, v, left);
+                    uint16_t *c = static_cast<uint16_t *>(p.c) + at;
+                    if (PAST && left >= 8) __builtin_nontemporal_store(v, &reinterpret_cast<Unit8 *>(c)->v);
+                    else store_unit8(c, v, left);
                 }
             }
+            ask_h(r0 / kRows + kAhead);
         }
     };
     // asks for the first stages of the tile that find() has set up
@@ -518,24 +559,31 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         if (stages > 0) {
             lanes_u32x4 a0[MI], b0[NI], a1[MI], b1[NI];
             land(std::integral_constant<int, kBuffers - 1>{});
+            // A wave whose part of the tile does not exist takes part in the loads and leaves the matrix cores to the others (forward 32768 x 4096
+            // x 2048 in 16 uneven groups: 515 us -> 499).
+            if (wm < now.rows && wn < now.cols) {
 #pragma unroll
-            for (int n = 0; n < MI + NI; ++n) read(0, 0, n, a0, b0);
-            for (int s = 0; s < stages; ++s) {
-                step(s, std::false_type{}, a0, b0, a1, b1);
-                step(s, std::true_type{}, a1, b1, a0, b0);
+                for (int n = 0; n < MI + NI; ++n) read(0, 0, n, a0, b0);
+                for (int s = 0; s < stages; ++s) {
+                    step(s, std::false_type{}, std::true_type{}, a0, b0, a1, b1);
+                    step(s, std::true_type{}, std::true_type{}, a1, b1, a0, b0);
+                }
+            } else {
+                for (int s = 0; s < stages; ++s) step(s, std::true_type{}, std::false_type{}, a1, b1, a0, b0);
             }
             land(std::integral_constant<int, 0>{});        // no wave reads the stages any more, no load is under way
         }
         if constexpr (!T::kLoops) {
-            leave(now);
+            leave(now, [] {});
             return;
         } else {
             // the next tile's first stages come in while this one's results leave
             GroupedOut next;
-            id += (int)gridDim.x;
-            stages = find(id, next);
-            if (stages > 0) start();
-            leave(now);
+            leave(now, [&] {
+                id += (int)gridDim.x;
+                stages = find(id, next);
+                if (stages > 0) start();
+            });
             if (stages < 0) return;
             now = next;
         }
@@ -557,11 +605,11 @@ static hipError_t ask_lds(int bytes)
     return e;
 }
 
-template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA, bool GATHER, bool OUT_F32>
-static hipError_t grouped_run(const GroupedProblem &q, hipStream_t st)
+template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA, bool GATHER, bool OUT_F32, bool PAST>
+static hipError_t grouped_launch(const GroupedProblem &q, hipStream_t st)
 {
     using T = GroupedTile<FORM, BM, BN, WM, WN, BUFFERS, DMA, GATHER, OUT_F32>;
-    constexpr auto kernel = grouped_kernel<T, FORM, BM, BN, WM, WN, OUT_F32>;
+    constexpr auto kernel = grouped_kernel<T, FORM, BM, BN, WM, WN, OUT_F32, PAST>;
     GroupedArgs a{q.E, q.M, q.out_rows, q.cols, q.red, q.offsets, q.rows, q.src_rows, reinterpret_cast<const char *>(q.a),
                   reinterpret_cast<const char *>(q.b), q.lda * 2, q.ldb * 2, q.c, q.ldc, q.accumulate, q.act, q.h, q.ldh, 0, 0};
     a.col_tiles = (q.cols + BN - 1) / BN;
@@ -584,6 +632,19 @@ static hipError_t grouped_run(const GroupedProblem &q, hipStream_t st)
         if (e != hipSuccess) return e;
     }
     return launch_kernel(kernel, dim3((unsigned)tiles), dim3(T::kThreads), T::kLds, st, a);
+}
+
+template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA, bool GATHER, bool OUT_F32>
+static hipError_t grouped_run(const GroupedProblem &q, hipStream_t st)
+{
+    // Results that no cache would hold until they are read go past the L2, which keeps the operands: gradients of weights, and what would fill the 256 MB
+    // of the last level.  dW of 16384 x 4096 x 2048 in 8 groups, to float32 265 us -> 246, to bfloat16 264 -> 242; forward 32768 x 4096 (268 MB) with
+    // reductions of 512, 189 -> 170, of 1024, 280 -> 241, of 2048, no difference; but dX of 32768 x 2048 (134 MB) by 512 71 -> 76.
+    const bool past = FORM == GROUPED_DW || (int64_t)q.M * q.cols * (OUT_F32 ? 4 : 2) > 192ll << 20;
+    if constexpr (FORM == GROUPED_DW || BM == 256)
+        if (past) return grouped_launch<FORM, BM, BN, WM, WN, BUFFERS, DMA, GATHER, OUT_F32, true>(q, st);
+    if constexpr (FORM != GROUPED_DW) return grouped_launch<FORM, BM, BN, WM, WN, BUFFERS, DMA, GATHER, OUT_F32, false>(q, st);
+    return hipErrorInvalidValue;        // not reached
 }
 
 template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA>
