@@ -74,6 +74,14 @@ __device__ __forceinline__ float group_sum(float x)
 #undef STEP
     return x;
 }
+// over a row of 16
+__device__ __forceinline__ uint32_t row_total(uint32_t x)
+{
+#define STEP(C) x += (uint32_t)dpp_of<C, 0xf>(0, (int)x);
+    POLYDL_ROW_STEPS(STEP)
+#undef STEP
+    return x;
+}
 
 // bfloat16 bits <-> float.  To bfloat16: round to nearest, ties to even; the compiler's conversion is one instruction a pair.
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __builtin_bit_cast(float, w << 16); }

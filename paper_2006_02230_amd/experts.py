@@ -88,9 +88,9 @@ def route(logits, k, renorm=True, stream=None):
     """polydl_route on float32 logits [T][E]: Route(ids [T][k], weights [T][k], offsets [E+1], tokens [T*k], slots [T][k])."""
     T, E = logits.shape
     src = _dense(logits, "logits", torch.float32, (T, E), _device())
-    ids, slots = _new((2, T, k), torch.int32, logits, stream).unbind(0)          # allocations take longer than views
+    ids, slots, weights = _new((3, T, k), torch.int32, logits, stream).unbind(0)          # allocations take longer than views
+    weights = weights.view(torch.float32)
     tokens, offsets = _new((T * k + E + 1,), torch.int32, logits, stream).split_with_sizes((T * k, E + 1))
-    weights = _new((T, k), torch.float32, logits, stream)
     need = lib.polydl_route_workspace_bytes(T, E) if T > 64 else 0
     space = _new((need,), torch.uint8, logits, stream) if need else None
     _check(lib.polydl_route(T, E, k, src, bool(renorm), ids.data_ptr(), weights.data_ptr(), offsets.data_ptr(), tokens.data_ptr(),
