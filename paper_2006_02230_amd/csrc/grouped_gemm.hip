@@ -255,7 +255,9 @@ __device__ __forceinline__ void gg_wait()
 }
 
 // four floats at any of their addresses
-struct __attribute__((packed, aligned(4))) Floats4 { gg_f32x4 v; };
+typedef gg_f32x4 __attribute__((aligned(4))) Floats4;
+// eight 16-bit values at any of theirs
+typedef lanes_u32x4 __attribute__((aligned(2))) Halves8;
 
 template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA, bool GATHER, bool OUT_F32>
 struct GroupedTile {
@@ -383,7 +385,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         else a[n - NI] = T::A::operand(buffer(s), wm, n - NI, kk, lane);
     };
     gg_f32x4 acc[MI][NI];
-    const auto step = [&](int s, auto half, auto busy, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI],
+    const auto step = [&](int s, auto half, auto busy, auto first, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI], lanes_u32x4 (&a_next)[MI],
                           lanes_u32x4 (&b_next)[NI]) {
         constexpr bool kSecond = decltype(half)::value, kBusy = decltype(busy)::value;
         if constexpr (kSecond) {
@@ -402,7 +404,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             // columns as the instruction's rows: a lane then holds four neighbouring columns of one row of the result
 #pragma unroll
             for (int j = 0; j < NI; ++j)
-                if constexpr (kBusy) acc[i][j] = gg_mfma(b[j], a[i], acc[i][j]);
+                if constexpr (kBusy) acc[i][j] = gg_mfma(b[j], a[i], decltype(first)::value ? gg_f32x4{0.f, 0.f, 0.f, 0.f} : acc[i][j]);
             if (kSecond && i == 0) {
                 A.begin(s + kBuffers, tid);
                 B.begin(s + kBuffers, tid);
@@ -429,15 +431,46 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
     // uneven groups with ReLU 313 us -> 301; without the activation 269.)
     constexpr int kChunks = WM / kRows, kPer = kRows * kAcrossUnits / 64, kWords = OUT_F32 ? 2 : 4;
     constexpr int kAhead = FORM != GROUPED_DX ? 1 : 32 / (kPer * kWords) < kChunks ? 32 / (kPer * kWords) : kChunks;
+    // The activation is a pass of its own: decided value by value, it came out as selects, six instructions a value, that ran without one too.  (With the
+    // first stage's zeros and one address a lane for whole tiles: forward 32768 x 4096 x 2048 in 16 groups 489 us -> 470.)  The maximum
+    // lets NaN through, as the formula does.
+    const auto activate = [&]() {
+        if (FORM != GROUPED_FWD || p.act == POLYDL_ACT_NONE) return;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_elementwise_maximum(acc[i][j], gg_f32x4{0.f, 0.f, 0.f, 0.f});
+        if (p.act != POLYDL_ACT_RELU6) return;
+#pragma unroll
+        for (int i = 0; i < MI; ++i)
+#pragma unroll
+            for (int j = 0; j < NI; ++j) acc[i][j] = __builtin_elementwise_minimum(acc[i][j], gg_f32x4{6.f, 6.f, 6.f, 6.f});
+    };
+    // zeros where the activation did not let through what gave x
+    const auto closed = [&](lanes_u32x4 v, lanes_u32x4 x) {
+        const float limit = p.act == POLYDL_ACT_RELU6 ? 6.f : __builtin_nanf("");
+#pragma unroll
+        for (int q = 0; q < kUnit; ++q) {
+            const float y = q & 1 ? bf16_hi(x[q >> 1]) : bf16_lo(x[q >> 1]);
+            const bool open = y > 0.f && !(y >= limit);
+            if constexpr (OUT_F32) v[q] = open ? v[q] : 0u;
+            else v[q >> 1] &= open ? 0xffffffffu : q & 1 ? 0x0000ffffu : 0xffff0000u;
+        }
+        return v;
+    };
     // go_on() starts the next tile
     const auto leave = [&](const GroupedOut &out, auto go_on) {
         // the compiler may not know that the lane is the same for every tile: it would keep all the addresses below in registers
         // through the products, and spill
         int lane = tid & 63;
         if constexpr (T::kLoops) asm volatile("" : "+v"(lane));
-        const bool early = FORM == GROUPED_DX && p.act != POLYDL_ACT_NONE && out.rows >= wm + WM && out.cols >= wn + WN && p.ldh < (1 << 24);
+        // a wave's part that is whole: one address a lane, the rest of it the same for the wave
+        const bool whole = wave_value((int)(out.rows >= wm + WM && out.cols >= wn + WN && p.ldc < (1 << 24) && p.ldh < (1 << 24)));
+        const bool early = FORM == GROUPED_DX && p.act != POLYDL_ACT_NONE && whole;
+        constexpr int kOutSize = OUT_F32 ? 4 : 2;
+        const uint64_t c_base = wave_value((uint64_t)p.c + (uint64_t)(out.c0 + (int64_t)wm * p.ldc + wn) * kOutSize);
+        const uint32_t c_off = (uint32_t)(lane / kAcrossUnits) * (uint32_t)(p.ldc * kOutSize) + (uint32_t)(lane % kAcrossUnits) * 16u;
         std::conditional_t<OUT_F32, gg_u32x2, lanes_u32x4> held_h[kAhead][kPer];
-        // one address a lane, the rest of it the same for the wave
         const uint64_t h_base = wave_value((uint64_t)(p.h + out.h0 + (int64_t)wm * p.ldh + wn));
         const uint32_t h_off = (uint32_t)(lane / kAcrossUnits) * (uint32_t)(p.ldh * 2) + (uint32_t)(lane % kAcrossUnits * kUnit) * 2u;
         const auto ask_h = [&](int chunk) {
@@ -457,60 +490,63 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
 #pragma unroll
         for (int i = 0; i < kAhead; ++i) ask_h(i);
         go_on();
+        activate();
 #pragma unroll
         for (int r0 = 0; r0 < WM; r0 += kRows) {
 #pragma unroll
             for (int i = 0; i < kRows / 16; ++i)
 #pragma unroll
                 for (int j = 0; j < NI; ++j) {
-                    gg_f32x4 v = acc[r0 / 16 + i][j];
-                    if constexpr (FORM == GROUPED_FWD) {
-#pragma unroll
-                        for (int q = 0; q < 4; ++q) {
-                            // comparisons that let NaN through, as the formula does
-                            if (p.act != POLYDL_ACT_NONE) v[q] = v[q] < 0.f ? 0.f : v[q];
-                            if (p.act == POLYDL_ACT_RELU6) v[q] = v[q] > 6.f ? 6.f : v[q];
-                        }
-                    }
+                    const gg_f32x4 v = acc[r0 / 16 + i][j];
                     const int r = i * 16 + (lane & 15), n = j * 16 + (lane >> 4) * 4;
                     char *at = mine + (r * kAcrossUnits + ((n / kUnit) ^ (r & kTwist))) * 16;
                     if constexpr (OUT_F32) *reinterpret_cast<gg_f32x4 *>(at) = v;
                     else *reinterpret_cast<gg_u32x2 *>(at + (n & 4) * 2) = gg_u32x2{bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
                 }
+            if (whole) {
 #pragma unroll
-            for (int i = 0; i < kRows * kAcrossUnits / 64; ++i) {
+                for (int i = 0; i < kPer; ++i) {
+                    constexpr int kStep = 64 / kAcrossUnits;
+                    const int r = i * kStep + lane / kAcrossUnits, u = lane % kAcrossUnits;
+                    lanes_u32x4 v = *reinterpret_cast<const lanes_u32x4 *>(mine + (r * kAcrossUnits + (u ^ (r & kTwist))) * 16);
+                    if (early) {
+                        const auto x = held_h[r0 / kRows % kAhead][i];
+                        if constexpr (OUT_F32) v = closed(v, lanes_u32x4{x[0], x[1], 0u, 0u});
+                        else v = closed(v, x);
+                    }
+                    char *c = reinterpret_cast<char *>(c_base + (uint64_t)((r0 + i * kStep) * kOutSize) * (uint64_t)p.ldc + c_off);
+                    if constexpr (OUT_F32) {
+                        Floats4 *at = reinterpret_cast<Floats4 *>(c);
+                        gg_f32x4 f = __builtin_bit_cast(gg_f32x4, v);
+                        if (p.accumulate) f += *at;
+                        if constexpr (PAST) __builtin_nontemporal_store(f, at);
+                        else *at = f;
+                    } else {
+                        Halves8 *at = reinterpret_cast<Halves8 *>(c);
+                        if constexpr (PAST) __builtin_nontemporal_store(v, at);
+                        else *at = v;
+                    }
+                }
+                ask_h(r0 / kRows + kAhead);
+                continue;
+            }
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
                 const int r = i * (64 / kAcrossUnits) + lane / kAcrossUnits, u = lane % kAcrossUnits;
                 const int row = wm + r0 + r, n = wn + u * kUnit, left = out.cols - n;
                 lanes_u32x4 v = *reinterpret_cast<const lanes_u32x4 *>(mine + (r * kAcrossUnits + (u ^ (r & kTwist))) * 16);
                 if (row >= out.rows || left <= 0) continue;
                 const int64_t at = out.c0 + (int64_t)row * p.ldc + n;
-                if constexpr (FORM == GROUPED_DX) {
-                    if (p.act != POLYDL_ACT_NONE) {
-                        lanes_u32x4 x;
-                        if (early) {
-                            const auto u = held_h[r0 / kRows % kAhead][i];
-                            if constexpr (OUT_F32) x = lanes_u32x4{u[0], u[1], 0u, 0u};
-                            else x = u;
-                        } else {
-                            const uint16_t *h = p.h + out.h0 + (int64_t)row * p.ldh + n;
-                            x = kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit), p.cols) : load_unit4(h);
-                        }
-#pragma unroll
-                        for (int q = 0; q < kUnit; ++q) {
-                            const float y = q & 1 ? bf16_hi(x[q >> 1]) : bf16_lo(x[q >> 1]);
-                            const bool open = y > 0.f && (p.act == POLYDL_ACT_RELU || y < 6.f);
-                            if constexpr (OUT_F32) v[q] = open ? v[q] : 0u;
-                            else v[q >> 1] &= open ? 0xffffffffu : q & 1 ? 0x0000ffffu : 0xffff0000u;
-                        }
-                    }
+                if (FORM == GROUPED_DX && p.act != POLYDL_ACT_NONE) {
+                    const uint16_t *h = p.h + out.h0 + (int64_t)row * p.ldh + n;
+                    v = closed(v, kUnit == 8 || left < 4 ? load_unit8(h, min(left, kUnit), p.cols) : load_unit4(h));
                 }
                 if constexpr (OUT_F32) {
                     float *c = static_cast<float *>(p.c) + at;
                     gg_f32x4 f = __builtin_bit_cast(gg_f32x4, v);
                     if (left >= 4) {
-                        if (p.accumulate) f += reinterpret_cast<const Floats4 *>(c)->v;
-                        if constexpr (PAST) __builtin_nontemporal_store(f, &reinterpret_cast<Floats4 *>(c)->v);
-                        else reinterpret_cast<Floats4 *>(c)->v = f;
+                        if (p.accumulate) f += *reinterpret_cast<const Floats4 *>(c);
+                        *reinterpret_cast<Floats4 *>(c) = f;
                     } else {
 #pragma unroll
                         for (int q = 0; q < 3; ++q)
@@ -518,11 +554,9 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
                     }
                 } else {
                     uint16_t *c = static_cast<uint16_t *>(p.c) + at;
-                    if (PAST && left >= 8) __builtin_nontemporal_store(v, &reinterpret_cast<Unit8 *>(c)->v);
-                    else store_unit8(c, v, left);
+                    store_unit8(c, v, left);
                 }
             }
-            ask_h(r0 / kRows + kAhead);
         }
     };
     // asks for the first stages of the tile that find() has set up
@@ -552,25 +586,39 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
     if (stages < 0) return;
     if (stages > 0) start();
     while (true) {
+        // A wave whose part of the tile does not exist takes part in the loads and leaves the matrix cores to the others (forward 32768 x 4096
+        // x 2048 in 16 uneven groups: 515 us -> 499).  The first half of the forward product's first stage adds to zeros that are in
+        // no register (the other forms' registers do not suffice for a first stage of its own: dW to bfloat16 239 us -> 251).
+        constexpr bool kPeeled = FORM == GROUPED_FWD;
+        const auto clear = [&]() {
 #pragma unroll
-        for (int i = 0; i < MI; ++i)
+            for (int i = 0; i < MI; ++i)
 #pragma unroll
-            for (int j = 0; j < NI; ++j) acc[i][j] = gg_f32x4{0.f, 0.f, 0.f, 0.f};
-        if (stages > 0) {
+                for (int j = 0; j < NI; ++j) acc[i][j] = gg_f32x4{0.f, 0.f, 0.f, 0.f};
+        };
+        if constexpr (!kPeeled) clear();
+        const bool busy = stages > 0 && wave_value((int)(wm < now.rows && wn < now.cols));
+        if (stages > 0) land(std::integral_constant<int, kBuffers - 1>{});
+        if (busy) {
             lanes_u32x4 a0[MI], b0[NI], a1[MI], b1[NI];
-            land(std::integral_constant<int, kBuffers - 1>{});
-            // A wave whose part of the tile does not exist takes part in the loads and leaves the matrix cores to the others (forward 32768 x 4096
-            // x 2048 in 16 uneven groups: 515 us -> 499).
-            if (wm < now.rows && wn < now.cols) {
+            constexpr std::true_type yes;
+            constexpr std::false_type no;
 #pragma unroll
-                for (int n = 0; n < MI + NI; ++n) read(0, 0, n, a0, b0);
-                for (int s = 0; s < stages; ++s) {
-                    step(s, std::false_type{}, std::true_type{}, a0, b0, a1, b1);
-                    step(s, std::true_type{}, std::true_type{}, a1, b1, a0, b0);
-                }
-            } else {
-                for (int s = 0; s < stages; ++s) step(s, std::true_type{}, std::false_type{}, a1, b1, a0, b0);
+            for (int n = 0; n < MI + NI; ++n) read(0, 0, n, a0, b0);
+            if constexpr (kPeeled) {
+                step(0, no, yes, yes, a0, b0, a1, b1);
+                step(0, yes, yes, no, a1, b1, a0, b0);
             }
+            for (int s = kPeeled ? 1 : 0; s < stages; ++s) {
+                step(s, no, yes, no, a0, b0, a1, b1);
+                step(s, yes, yes, no, a1, b1, a0, b0);
+            }
+        } else {
+            if constexpr (kPeeled) clear();
+            lanes_u32x4 a[MI], b[NI];
+            for (int s = 0; s < stages; ++s) step(s, std::true_type{}, std::false_type{}, std::false_type{}, a, b, a, b);
+        }
+        if (stages > 0) {
             land(std::integral_constant<int, 0>{});        // no wave reads the stages any more, no load is under way
         }
         if constexpr (!T::kLoops) {
