@@ -382,6 +382,54 @@ def test_gradient_of_weights_over_long_groups(P, N, K, how):
         close(got[e], dy[a:b].double().T @ xs[a:b], dy[a:b].double().abs().T @ xs[a:b].abs(), counts[e], e)
 
 
+# groups of tiles of 256: whole and partial ones, groups that end in few rows, empty ones, rows behind the last; results too large for any cache
+LARGE = [((1500, 77, 0, 2300, 300), 40, 2056, 136), ((30000, 19000, 159), 0, 2056, 64)]
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("act", [None, "relu", "relu6"])
+@pytest.mark.parametrize("counts,tail,N,K", LARGE, ids=["partial", "past"])
+def test_grouped_forward_in_large_tiles(P, counts, tail, N, K, act, dtype):
+    import torch
+    E = len(counts)
+    offsets, M = ragged(counts, tail)
+    g = gen(31)
+    x, w = randn(g, M, K).bfloat16(), (randn(g, E, N, K) * 3 * K ** -0.5).bfloat16()
+    broken = [5, offsets[1] - 1, offsets[-1] - 1]                     # in a whole tile, in partial ones
+    x[broken] = float("nan")
+    got = P.grouped_gemm_bf16(x, w, ints(offsets), act=act, out_dtype=getattr(torch, dtype))
+    assert bool(torch.isnan(got[broken]).all())
+    got[broken] = 0.0
+    x[broken] = 0.0
+    assert bool((got[offsets[-1]:] == 0).all())
+    for e in range(E):
+        a, b = offsets[e], offsets[e + 1]
+        want, mag = x[a:b].double() @ w[e].double().T, x[a:b].double().abs() @ w[e].double().abs().T
+        want = want if act is None else want.clamp(min=0) if act == "relu" else want.clamp(0, 6)
+        close(got[a:b], want, mag, K, (e, act, dtype))
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("act", [None, "relu", "relu6"])
+@pytest.mark.parametrize("counts,tail,K,N", LARGE, ids=["partial", "past"])
+def test_grouped_gradient_of_rows_in_large_tiles(P, counts, tail, K, N, act, dtype):
+    import torch
+    E = len(counts)
+    offsets, M = ragged(counts, tail)
+    g = gen(32)
+    dy, w = randn(g, M, N).bfloat16(), (randn(g, E, N, K) * N ** -0.5).bfloat16()
+    h = (randn(g, M, K) * 4).bfloat16()                               # negative ones, infinities and NaN among them: closed, open (ReLU), closed
+    h[7, 3::50], h[offsets[1] - 1, 1::50] = float("inf"), float("nan")
+    got = P.grouped_gemm_dx_bf16(dy, w, ints(offsets), h=h, act=act, out_dtype=getattr(torch, dtype))
+    assert bool((got[offsets[-1]:] == 0).all())
+    for e in range(E):
+        a, b = offsets[e], offsets[e + 1]
+        want, mag = dy[a:b].double() @ w[e].double(), dy[a:b].double().abs() @ w[e].double().abs()
+        if act is not None:
+            want = torch.where((h[a:b] > 0) & ((h[a:b] < 6) if act == "relu6" else True), want, 0.0)
+        close(got[a:b], want, mag, N, (e, act, dtype))
+
+
 def test_grouped_infinities_stay_in_their_rows(P):
     import torch
     offsets, M = ragged((70, 60), 0)
