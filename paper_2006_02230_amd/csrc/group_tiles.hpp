@@ -16,6 +16,21 @@ __device__ __forceinline__ GroupRows group_rows(const int32_t *offsets, int e, i
     return {lo, hi};
 }
 
+// The group that comes turn-th by length, the longest first, the lower first among equal ones; of at most kSorted groups (more even out by themselves).
+constexpr int kSorted = 32;
+__device__ __forceinline__ int by_length(const int32_t *offsets, int turn, int E, int M)
+{
+    const int lane = threadIdx.x & 63;
+    const GroupRows g = group_rows(offsets, min(lane, E), E, M);
+    const int length = lane < E ? g.hi - g.lo : -1;
+    int before = lane < E ? 0 : -1;
+    for (int i = 0; i < E; ++i) {
+        const int other = lane_of(length, i);
+        before += other > length || (other == length && i < lane);
+    }
+    return __builtin_ctzll(__ballot(lane < E && before == turn));
+}
+
 // Consecutive workgroups go to the eight dies in turn: die x takes the x-th eighth of the tiles, so that the tiles that
 // share operands share an L2.
 __device__ __forceinline__ int die_order(int id, int total)
