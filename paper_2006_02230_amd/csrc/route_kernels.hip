@@ -17,10 +17,10 @@
 namespace polydl {
 
 // A float as an unsigned key of the same order; 0 for -infinity (a masked logit is never taken), all ones for NaN (taken
-// first: a broken logit shows in the weights rather than being dropped).
+// first: a broken logit shows in the weights rather than being dropped).  Adding zero makes -0 the +0 that it is equal to.
 __device__ __forceinline__ uint32_t route_key(float v)
 {
-    const uint32_t u = __builtin_bit_cast(uint32_t, v);
+    const uint32_t u = __builtin_bit_cast(uint32_t, v + 0.f);
     const uint32_t key = u ^ ((uint32_t)((int)u >> 31) | 0x80000000u);
     return v != v ? 0xffffffffu : v == -INFINITY ? 0u : key;
 }
