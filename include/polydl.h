@@ -258,7 +258,7 @@ int polydl_activation(int64_t count, float *y, int act, void *stream);
  * The plan stays in device memory: no entry point here waits for the device or needs to know the groups' sizes.  None keeps memory
  * of its own (route takes a workspace), and all may be captured.  Results do not depend on the run: sums have a fixed order.
  * bfloat16 values are uint16_t bit patterns, products of them exact, sums float32, each result rounded once to nearest even.
- * Row strides (ld...) count elements and may exceed the row.  Any size, alignment to an element and stride is served; the products are fast
+ * Row strides (ld...) count elements and may exceed the row.  Any alignment to an element, any stride and sizes E, M, N and K up to 2^31 - 2^16 are served; the products are fast
  * where K, N and the strides are multiples of 8 and the tensors 16-byte aligned.  A pointer to a tensor without
  * elements may be NULL.  Errors: POLYDL_ERR_BAD_DIMENSION for a size or stride out of range, POLYDL_ERR_UNSUPPORTED for an
  * activation, type, alignment or size that no kernel serves.

@@ -11,6 +11,10 @@ bool aligned(const void *p, uintptr_t bytes) { return ((uintptr_t)p & (bytes - 1
 bool any_act(int act) { return act == POLYDL_ACT_NONE || act == POLYDL_ACT_RELU || act == POLYDL_ACT_RELU6; }
 bool any_type(int type) { return type == POLYDL_F32 || type == POLYDL_BF16; }
 bool aligned_type(const void *p, int type) { return aligned(p, type == POLYDL_F32 ? 4 : 2); }
+// Lengths (groups, slots, columns, reductions) whose last tile, the stages asked for past their end and the row indices kept in LDS
+// stay within the kernels' 32-bit arithmetic.
+constexpr int kMaxLength = 0x7fff0000;
+bool too_long(int E, int M, int N, int K) { return E > kMaxLength || M > kMaxLength || N > kMaxLength || K > kMaxLength; }
 // element counts whose byte offsets a 64-bit product holds with room to spare
 constexpr int64_t kMaxElements = 1ll << 60, kMaxRowStride = 1ll << 40;
 bool too_many(int64_t a, int64_t b, int64_t c) { return (__int128)a * b * c >= kMaxElements; }
@@ -89,7 +93,8 @@ int polydl_grouped_gemm_bf16(int E, int M, int N, int K, const int32_t *offsets,
 {
     if (E <= 0 || M < 0 || N <= 0 || K <= 0 || ldx < K || ldy < N || x_rows < 0 || (!rows && x_rows != M)) return POLYDL_ERR_BAD_DIMENSION;
     if (!offsets || !w || (M > 0 && ((x_rows > 0 && !x) || !y))) return POLYDL_ERR_NULL_POINTER;
-    if (!any_act(act) || !any_type(out_type) || ldx > kMaxRowStride || ldy > kMaxRowStride || too_many(E, N, K)) return POLYDL_ERR_UNSUPPORTED;
+    if (!any_act(act) || !any_type(out_type) || ldx > kMaxRowStride || ldy > kMaxRowStride || too_long(E, M, N, K) || too_many(E, N, K))
+        return POLYDL_ERR_UNSUPPORTED;
     if (!aligned(offsets, 4) || !aligned(rows, 4) || !aligned(x, 2) || !aligned(w, 2) || !aligned_type(y, out_type)) return POLYDL_ERR_UNSUPPORTED;
     if (!on_gfx950()) return POLYDL_ERR_NO_DEVICE;
     if (M == 0) return POLYDL_OK;
@@ -107,7 +112,8 @@ int polydl_grouped_gemm_dx_bf16(int E, int M, int N, int K, const int32_t *offse
 {
     if (E <= 0 || M < 0 || N <= 0 || K <= 0 || lddy < N || lddx < K || (act != POLYDL_ACT_NONE && ldh < K)) return POLYDL_ERR_BAD_DIMENSION;
     if (!offsets || !w || (M > 0 && (!dy || !dx || (act != POLYDL_ACT_NONE && !h)))) return POLYDL_ERR_NULL_POINTER;
-    if (!any_act(act) || !any_type(out_type) || lddy > kMaxRowStride || lddx > kMaxRowStride || ldh > kMaxRowStride || too_many(E, N, K))
+    if (!any_act(act) || !any_type(out_type) || lddy > kMaxRowStride || lddx > kMaxRowStride || ldh > kMaxRowStride ||
+        too_long(E, M, N, K) || too_many(E, N, K))
         return POLYDL_ERR_UNSUPPORTED;
     if (!aligned(offsets, 4) || !aligned(dy, 2) || !aligned(w, 2) || !aligned(h, 2) || !aligned_type(dx, out_type)) return POLYDL_ERR_UNSUPPORTED;
     if (!on_gfx950()) return POLYDL_ERR_NO_DEVICE;
@@ -127,7 +133,8 @@ int polydl_grouped_gemm_dw_bf16(int E, int M, int N, int K, const int32_t *offse
 {
     if (E <= 0 || M < 0 || N <= 0 || K <= 0 || lddy < N || ldx < K || x_rows < 0 || (!rows && x_rows != M)) return POLYDL_ERR_BAD_DIMENSION;
     if (!offsets || !dw || (M > 0 && (!dy || (x_rows > 0 && !x)))) return POLYDL_ERR_NULL_POINTER;
-    if (!any_type(out_type) || (accumulate && out_type != POLYDL_F32) || lddy > kMaxRowStride || ldx > kMaxRowStride || too_many(E, N, K))
+    if (!any_type(out_type) || (accumulate && out_type != POLYDL_F32) || lddy > kMaxRowStride || ldx > kMaxRowStride ||
+        too_long(E, M, N, K) || too_many(E, N, K))
         return POLYDL_ERR_UNSUPPORTED;
     if (!aligned(offsets, 4) || !aligned(rows, 4) || !aligned(dy, 2) || !aligned(x, 2) || !aligned_type(dw, out_type)) return POLYDL_ERR_UNSUPPORTED;
     if (!on_gfx950()) return POLYDL_ERR_NO_DEVICE;
@@ -147,7 +154,7 @@ int polydl_w4_pack_bf16(int E, int N, int K, int group, const uint16_t *w, uint8
 {
     if (E <= 0 || N <= 0 || K <= 0) return POLYDL_ERR_BAD_DIMENSION;
     if (!w || !q || !scales) return POLYDL_ERR_NULL_POINTER;
-    if (!w4_group(group) || K > 0x7fffff00 || N > 0x7fffff00 || too_many(E, (int64_t)N + 15, (int64_t)K + 127)) return POLYDL_ERR_UNSUPPORTED;
+    if (!w4_group(group) || too_long(E, 0, N, K) || too_many(E, (int64_t)N + 15, (int64_t)K + 127)) return POLYDL_ERR_UNSUPPORTED;
     if (!aligned(w, 2) || !aligned(q, 16) || !aligned(scales, 8)) return POLYDL_ERR_UNSUPPORTED;
     if (!on_gfx950()) return POLYDL_ERR_NO_DEVICE;
     return launched_or_refused(w4_pack_launch(E, N, K, group, w, q, scales, zeros, (hipStream_t)stream));
@@ -159,8 +166,8 @@ int polydl_w4_gemm_bf16(int E, int M, int N, int K, int group, const int32_t *of
 {
     if (E <= 0 || M < 0 || N <= 0 || K <= 0 || ldx < K || ldy < N || x_rows < 0 || (!rows && x_rows != M)) return POLYDL_ERR_BAD_DIMENSION;
     if ((E > 1 && !offsets) || !q || !scales || (M > 0 && ((x_rows > 0 && !x) || !y))) return POLYDL_ERR_NULL_POINTER;
-    if (!w4_group(group) || !any_act(act) || !any_type(out_type) || ldx > kMaxRowStride || ldy > kMaxRowStride || K > 0x7fffff00 ||
-        N > 0x7fffff00 || too_many(E, (int64_t)N + 15, (int64_t)K + 127))
+    if (!w4_group(group) || !any_act(act) || !any_type(out_type) || ldx > kMaxRowStride || ldy > kMaxRowStride || too_long(E, M, N, K) ||
+        too_many(E, (int64_t)N + 15, (int64_t)K + 127))
         return POLYDL_ERR_UNSUPPORTED;
     if (!aligned(offsets, 4) || !aligned(rows, 4) || !aligned(x, 2) || !aligned(q, 16) || !aligned(scales, 8) ||
         !aligned_type(y, out_type))

@@ -254,7 +254,7 @@ static hipError_t few_rows_run(const FewRowsProblem &p, hipStream_t st)
 template <class W>
 static hipError_t few_rows_pick(const FewRowsProblem &p, hipStream_t st)
 {
-    const int rows = (p.M + p.E - 1) / p.E;            // of a group, in the mean
+    const int64_t rows = ((int64_t)p.M + p.E - 1) / p.E;     // of a group, in the mean
     if (rows <= 16) {
         // Two tiles of outputs share the rows' loads; with fewer workgroups than compute units that costs more than it saves (one row, 4096 x
         // 4096 in 4 bits: 4.6 us with one tile, 5.5 with two; 32 rows of 64 experts, 2048 x 4096: 38 and 34).  Four waves take longer over a

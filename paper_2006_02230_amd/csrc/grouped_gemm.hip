@@ -673,7 +673,7 @@ static hipError_t grouped_launch(const GroupedProblem &q, hipStream_t st)
         const int64_t groups = q.M < q.E + 1 ? q.M : q.E + 1;
         tiles = (q.M + groups * (BM - 1)) / BM * a.col_tiles;
     }
-    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+    if (tiles > 0x7fff0000) return hipErrorInvalidValue;       // and a tile's number plus the workgroups is an int too
     if (T::kLoops) {
         const int64_t fit = (int64_t)compute_units() * (160 * 1024 / T::kLds);
         if (tiles > fit) tiles = fit;

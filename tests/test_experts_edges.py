@@ -1,0 +1,45 @@
+"""The layer of experts where it is easily wrong, on a machine without a GPU: sizes at the edge of 32 bits, memory for another
+stream, gradients that nobody would get, forwards without their backward."""
+import pytest
+
+import paper_2006_02230_amd as P
+
+OK, NULL, DIM, UNSUPPORTED, NO_DEVICE = 0, -1, -2, -3, -5
+AT = 4096          # an address that is aligned and never looked at
+MOST = (1 << 31) - (1 << 16)
+BIG = (1 << 31) - 1
+
+
+def st(name, *args):
+    return getattr(P.lib, name)(*args, None)
+
+
+def fwd(E=2, M=8, N=16, K=24):
+    return st("polydl_grouped_gemm_bf16", E, M, N, K, AT, None, M, AT, K, AT, AT, N, 1, 0)
+
+
+def dx(E=2, M=8, N=16, K=24):
+    return st("polydl_grouped_gemm_dx_bf16", E, M, N, K, AT, AT, N, AT, AT, K, 1, AT, K, 1)
+
+
+def dw(E=2, M=8, N=16, K=24):
+    return st("polydl_grouped_gemm_dw_bf16", E, M, N, K, AT, AT, N, None, M, AT, K, AT, 0, 0)
+
+
+def w4(E=2, M=8, N=16, K=24):
+    return st("polydl_w4_gemm_bf16", E, M, N, K, 32, AT, None, M, AT, K, AT, AT, AT, AT, N, 1, 0)
+
+
+def pack(E=2, N=16, K=24):
+    return st("polydl_w4_pack_bf16", E, N, K, 32, AT, AT, AT, AT)
+
+
+@pytest.mark.parametrize("f,names", [(fwd, "EMNK"), (dx, "EMNK"), (dw, "EMNK"), (w4, "EMNK"), (pack, "ENK")])
+def test_lengths_past_the_kernels_arithmetic_are_refused(f, names):
+    # a tile, a stage or a window of row indices that begins before the end may end past 2^31
+    import torch
+    for name in names:
+        for n in (MOST + 1, BIG - 300, BIG):
+            assert f(**{name: n}) == UNSUPPORTED, (f.__name__, name, n)
+        if not torch.cuda.is_available():
+            assert f(**{name: MOST}) == NO_DEVICE, (f.__name__, name)
