@@ -2,7 +2,10 @@
 with 4-bit weights (same names as the C entry points, argument marshalling only), and a layer that runs them together.
 
 Rows sorted by expert, their offsets, `tokens` and `slots` are tensors on the device (`route` makes them); nothing here waits for the
-device.  Matrices may have any row stride; their columns are contiguous."""
+device.  Matrices may have any row stride; their columns are contiguous.
+
+`stream` (None: torch's current stream) is where a call runs.  What it allocates is that stream's memory; as with any work on several streams, the
+caller makes `stream` wait for the arguments, keeps them until it has read them, and waits for it before using the results elsewhere."""
 import collections
 import ctypes
 
@@ -71,10 +74,13 @@ def _matrix(t, name, dtype, shape, dev):
 
 
 def _new(shape, dtype, like, stream):
-    """A tensor for a call on `stream` (None: torch's current one, on which it is allocated)."""
-    t = like.new_empty(shape, dtype=dtype)
-    if stream is not None:
-        t.record_stream(stream)
+    """A tensor for a call on `stream` (None: torch's current one).  It comes from the memory of that stream, whose work is in order: what
+    the current stream has freed may still be in use there.  The current stream, where results are read, is recorded on it."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(torch.cuda.current_stream())
     return t
 
 

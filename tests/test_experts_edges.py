@@ -43,3 +43,40 @@ def test_lengths_past_the_kernels_arithmetic_are_refused(f, names):
             assert f(**{name: n}) == UNSUPPORTED, (f.__name__, name, n)
         if not torch.cuda.is_available():
             assert f(**{name: MOST}) == NO_DEVICE, (f.__name__, name)
+
+
+class Recorder:
+    """Stands in for a tensor, torch's streams and its allocator; writes down who allocates where."""
+
+    def __init__(self, monkeypatch):
+        import contextlib
+
+        import torch
+        self.at, self.log = "current", []
+
+        @contextlib.contextmanager
+        def on(stream):
+            before, self.at = self.at, stream
+            yield
+            self.at = before
+        monkeypatch.setattr(torch.cuda, "stream", on)
+        monkeypatch.setattr(torch.cuda, "current_stream", lambda *a: self.at)
+
+    def new_empty(self, shape, dtype=None):
+        self.log.append(("empty", self.at))
+        return self
+
+    def record_stream(self, stream):
+        self.log.append(("record", stream))
+
+
+def test_memory_for_another_stream_is_that_streams(monkeypatch):
+    # memory of the current stream may be under work queued there, which a call on another stream does not wait for
+    import torch
+    from paper_2006_02230_amd import experts
+    like = Recorder(monkeypatch)
+    experts._new((3,), torch.float32, like, "side")
+    assert like.log == [("empty", "side"), ("record", "current")] and like.at == "current"
+    like.log.clear()
+    experts._new((3,), torch.float32, like, None)
+    assert like.log == [("empty", "current")]

@@ -45,3 +45,40 @@ def test_zeros_of_either_sign_are_equal_logits(P, T, E, k, renorm):
         assert np.array_equal(got.cpu().numpy(), want)
     # a difference of logits of at most 2, exponentials, a sum, a quotient
     assert (np.abs(r.weights.cpu().numpy() - w) <= w * (2 * 2 + 8 + 16 + E / 64) * 2.0 ** -23).all()
+
+
+# ---- another stream ----------------------------------------------------------------------------------------------
+
+def test_calls_on_another_stream_leave_the_current_streams_memory_alone(P):
+    # blocks that the current stream has freed, of every result's size, while its work may still use them: no result lies in one
+    import torch
+    g = gen(3)
+    T, E, k, D, F = 500, 16, 4, 128, 192
+    x, logits, w1 = randn(g, T, D).bfloat16(), randn(g, T, E), randn(g, E, F, D).bfloat16()
+    side = torch.cuda.Stream()
+    calls = {}
+
+    def run(stream):
+        r = calls["route"] = P.route(logits, k, stream=stream)
+        h = calls["forward"] = P.grouped_gemm_bf16(x, w1, r.offsets, rows=r.tokens, stream=stream)
+        calls["combine"] = P.combine_bf16(h, r.slots, r.weights, stream=stream)
+        calls["combine_bwd"] = P.combine_bwd_bf16(calls["combine"], h, r.slots, r.weights, stream=stream)
+        calls["dx"] = P.grouped_gemm_dx_bf16(h, w1, r.offsets, stream=stream)
+        calls["dw"] = P.grouped_gemm_dw_bf16(h, x, r.offsets, rows=r.tokens, stream=stream)
+        calls["route_bwd"] = P.route_bwd(logits, r.ids, r.weights, r.weights, stream=stream)
+        q = calls["pack"] = P.w4_pack_bf16(w1, 128, True, stream=stream)
+        calls["w4"] = P.w4_gemm_bf16(x, q.q, q.scales, F, 128, zeros=q.zeros, offsets=r.offsets, rows=r.tokens, stream=stream)
+        return {(name, i): t for name, v in calls.items() for i, t in enumerate((v,) if isinstance(v, torch.Tensor) else v)}
+
+    want = run(None)
+    torch.cuda.synchronize()
+    freed = [(t.untyped_storage().data_ptr(), t.untyped_storage().nbytes()) for t in want.values()]
+    values = {name: t.clone() for name, t in want.items()}
+    calls.clear()
+    del want
+    got = run(side)
+    side.synchronize()
+    for name, t in got.items():
+        at = t.untyped_storage().data_ptr()
+        assert not any(a < at + t.untyped_storage().nbytes() and at < a + n for a, n in freed), name
+        assert torch.equal(t.reshape(-1).view(torch.uint8), values[name].reshape(-1).view(torch.uint8)), name
