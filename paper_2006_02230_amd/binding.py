@@ -1,4 +1,7 @@
-"""ctypes binding of libpolydl.so: same names as the C entry points, argument marshalling only."""
+"""ctypes binding of libpolydl.so: same names as the C entry points, argument marshalling only.
+
+`stream` (None: torch's current stream) is where a call runs.  What it allocates is that stream's memory; as with any work on several streams, the
+caller makes `stream` wait for the arguments, keeps them until it has read them, and waits for it before using the results elsewhere."""
 import ctypes
 import os
 
@@ -151,6 +154,17 @@ def _stream_ptr(stream=None):
     return _raw_stream(_current_device())
 
 
+def _new(shape, dtype, like, stream):
+    """A tensor for a call on `stream` (None: torch's current one).  It comes from the memory of that stream, whose work is in order: what
+    the current stream has freed may still be in use there.  The current stream, where results are read, is recorded on it."""
+    if stream is None or not like.is_cuda:           # (what is no device tensor is refused later)
+        return like.new_empty(shape, dtype=dtype)
+    with torch.cuda.stream(stream):
+        t = like.new_empty(shape, dtype=dtype)
+    t.record_stream(torch.cuda.current_stream())
+    return t
+
+
 def _dev(t, name):
     """Device pointer of a contiguous float32 CUDA/HIP tensor (None passes NULL)."""
     if t is None:
@@ -171,7 +185,7 @@ def nchw_to_nchwc_bf16(x, b=8, stream=None, out=None):
     """polydl_nchw_to_nchwc_bf16 on a 16-bit NCHW tensor: returns [N][ceil(C/b)][H][W][b]."""
     N, C, H, W = x.shape
     if out is None:
-        out = torch.empty((N, -(-C // b), H, W, b), dtype=x.dtype, device=x.device)
+        out = _new((N, -(-C // b), H, W, b), x.dtype, x, stream)
     elif tuple(out.shape) != (N, -(-C // b), H, W, b) or out.dtype != x.dtype:
         raise ValueError("out must be a [N][ceil(C/b)][H][W][b] tensor of the input's type")
     _check(lib.polydl_nchw_to_nchwc_bf16(N, C, H, W, b, _dev16(x, "x"), _dev16(out, "out"), _stream_ptr(stream)),
@@ -183,7 +197,7 @@ def kcrs_to_kcrsck_bf16(w, bc=8, bk=1, stream=None, out=None):
     """polydl_kcrs_to_kcrsck_bf16: returns [ceil(K/bk)][ceil(C/bc)][R][S][bc][bk] (16-bit elements)."""
     K, C, R, S = w.shape
     if out is None:
-        out = torch.empty((-(-K // bk), -(-C // bc), R, S, bc, bk), dtype=w.dtype, device=w.device)
+        out = _new((-(-K // bk), -(-C // bc), R, S, bc, bk), w.dtype, w, stream)
     elif tuple(out.shape) != (-(-K // bk), -(-C // bc), R, S, bc, bk) or out.dtype != w.dtype:
         raise ValueError("out must be a [ceil(K/bk)][ceil(C/bc)][R][S][bc][bk] tensor of the input's type")
     _check(lib.polydl_kcrs_to_kcrsck_bf16(K, C, R, S, bc, bk, _dev16(w, "w"), _dev16(out, "out"),
@@ -198,7 +212,7 @@ def conv2d_fwd_bf16_blocked(x8c, w8c, C, bias=None, out=None, stride=1, pad=0, a
     P = (H + 2 * pad - R) // stride + 1
     Q = (W + 2 * pad - S) // stride + 1
     if out is None:
-        out = torch.empty((N, K, max(P, 0), max(Q, 0)), dtype=torch.float32, device=x8c.device)
+        out = _new((N, K, max(P, 0), max(Q, 0)), torch.float32, x8c, stream)
     st = lib.polydl_conv2d_fwd_bf16_blocked(N, C, H, W, K, R, S, stride, pad, _dev16(x8c, "x8c"),
                                             _dev16(w8c, "w8c"), _dev(bias, "bias"), _dev(out, "out"), ACT[act],
                                             _stream_ptr(stream))
@@ -214,9 +228,9 @@ def conv2d_fwd_bf16(x, w, bias=None, out=None, stride=1, pad=0, act=None, worksp
     Q = (W + 2 * pad - S) // stride + 1
     need = lib.polydl_conv2d_bf16_workspace_bytes(N, C, H, W, K, R, S)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _new(need, torch.uint8, x, stream)
     if out is None:
-        out = torch.empty((N, K, max(P, 0), max(Q, 0)), dtype=torch.float32, device=x.device)
+        out = _new((N, K, max(P, 0), max(Q, 0)), torch.float32, x, stream)
     st = lib.polydl_conv2d_fwd_bf16(N, C, H, W, K, R, S, stride, pad, _dev16(x, "x"), _dev16(w, "w"),
                                     _dev(bias, "bias"), _dev(out, "out"), ACT[act],
                                     workspace.data_ptr(), workspace.numel(), _stream_ptr(stream))
@@ -242,7 +256,7 @@ def conv2d_fwd(x, w, bias=None, out=None, stride=1, pad=0, act=None, stream=None
     P = (H + 2 * pad - R) // stride + 1
     Q = (W + 2 * pad - S) // stride + 1
     if out is None:
-        out = torch.empty((N, K, max(P, 0), max(Q, 0)), dtype=torch.float32, device=x.device)
+        out = _new((N, K, max(P, 0), max(Q, 0)), torch.float32, x, stream)
     if w_tap is not None:
         if pre_act is not None:
             raise ValueError("w_tap and pre_act do not combine")
@@ -296,7 +310,7 @@ def nchw_to_nchwc(x, b, stream=None, out=None):
     """polydl_nchw_to_nchwc: returns the [N][ceil(C/b)][H][W][b] tensor (written into out if given)."""
     N, C, H, W = x.shape
     if out is None:
-        out = torch.empty((N, -(-C // b), H, W, b), dtype=torch.float32, device=x.device)
+        out = _new((N, -(-C // b), H, W, b), torch.float32, x, stream)
     _check(lib.polydl_nchw_to_nchwc(N, C, H, W, b, _dev(x, "x"), _dev(out, "out"), _stream_ptr(stream)),
            "polydl_nchw_to_nchwc")
     return out
@@ -306,7 +320,7 @@ def nchwc_to_nchw(xb, C, stream=None, out=None):
     """polydl_nchwc_to_nchw: returns the [N][C][H][W] tensor (written into out if given)."""
     N, Cb, H, W, b = xb.shape
     if out is None:
-        out = torch.empty((N, C, H, W), dtype=torch.float32, device=xb.device)
+        out = _new((N, C, H, W), torch.float32, xb, stream)
     _check(lib.polydl_nchwc_to_nchw(N, C, H, W, b, _dev(xb, "xb"), _dev(out, "out"), _stream_ptr(stream)),
            "polydl_nchwc_to_nchw")
     return out
@@ -316,7 +330,7 @@ def kcrs_to_kcrsck(w, bc, bk, stream=None, out=None):
     """polydl_kcrs_to_kcrsck: returns the [ceil(K/bk)][ceil(C/bc)][R][S][bc][bk] tensor (out if given)."""
     K, C, R, S = w.shape
     if out is None:
-        out = torch.empty((-(-K // bk), -(-C // bc), R, S, bc, bk), dtype=torch.float32, device=w.device)
+        out = _new((-(-K // bk), -(-C // bc), R, S, bc, bk), torch.float32, w, stream)
     _check(lib.polydl_kcrs_to_kcrsck(K, C, R, S, bc, bk, _dev(w, "w"), _dev(out, "out"), _stream_ptr(stream)),
            "polydl_kcrs_to_kcrsck")
     return out
@@ -333,7 +347,7 @@ def bnorm_fwd(x, gamma, beta, mean, var, eps=1e-5, out=None, act=None, stream=No
     """polydl_bnorm_fwd on an NKPQ tensor; out defaults to a new tensor (pass out=x for in place)."""
     N, K, P, Q = x.shape
     if out is None:
-        out = torch.empty_like(x)
+        out = _new(x.shape, x.dtype, x, stream)
     st = lib.polydl_bnorm_fwd(N, K, P, Q, _dev(x, "x"), _dev(gamma, "gamma"), _dev(beta, "beta"), _dev(mean, "mean"),
                               _dev(var, "var"), ctypes.c_float(eps), _dev(out, "out"), ACT[act], _stream_ptr(stream))
     _check(st, "polydl_bnorm_fwd")

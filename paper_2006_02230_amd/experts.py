@@ -11,7 +11,7 @@ import ctypes
 
 import torch
 
-from .binding import ACT, _check, _current_device, _stream_ptr, lib
+from .binding import ACT, _check, _current_device, _new, _stream_ptr, lib
 
 _i, _p, _l, _z = ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t
 for _name, _args in {
@@ -71,17 +71,6 @@ def _matrix(t, name, dtype, shape, dev):
     if col != 1 and shape[1] > 1:
         raise TypeError("%s must have contiguous columns" % name)
     return t.data_ptr(), row if shape[0] > 1 else shape[1]
-
-
-def _new(shape, dtype, like, stream):
-    """A tensor for a call on `stream` (None: torch's current one).  It comes from the memory of that stream, whose work is in order: what
-    the current stream has freed may still be in use there.  The current stream, where results are read, is recorded on it."""
-    if stream is None:
-        return like.new_empty(shape, dtype=dtype)
-    with torch.cuda.stream(stream):
-        t = like.new_empty(shape, dtype=dtype)
-    t.record_stream(torch.cuda.current_stream())
-    return t
 
 
 def _type(dtype):

@@ -52,7 +52,7 @@ class Recorder:
         import contextlib
 
         import torch
-        self.at, self.log = "current", []
+        self.at, self.log, self.is_cuda = "current", [], True
 
         @contextlib.contextmanager
         def on(stream):
@@ -80,3 +80,28 @@ def test_memory_for_another_stream_is_that_streams(monkeypatch):
     like.log.clear()
     experts._new((3,), torch.float32, like, None)
     assert like.log == [("empty", "current")]
+
+
+def test_every_call_allocates_for_its_stream(monkeypatch):
+    import torch
+    from paper_2006_02230_amd import binding
+
+    class Allocated(Exception):
+        pass
+
+    def new(shape, dtype, like, stream):
+        raise Allocated(stream)
+    monkeypatch.setattr(binding, "_new", new)
+    f, h = torch.zeros, torch.bfloat16
+    calls = [lambda s: P.nchw_to_nchwc_bf16(f(1, 8, 4, 4, dtype=h), stream=s), lambda s: P.kcrs_to_kcrsck_bf16(f(8, 8, 1, 1, dtype=h), stream=s),
+             lambda s: P.conv2d_fwd_bf16_blocked(f(1, 1, 4, 4, 8, dtype=h), f(8, 1, 1, 1, 8, 1, dtype=h), 8, stream=s),
+             lambda s: P.conv2d_fwd_bf16(f(1, 8, 4, 4, dtype=h), f(8, 8, 1, 1, dtype=h), stream=s),
+             lambda s: P.conv2d_fwd_bf16(f(1, 8, 4, 4, dtype=h), f(8, 8, 1, 1, dtype=h), workspace=f(1), stream=s),
+             lambda s: P.conv2d_fwd(f(1, 8, 4, 4), f(8, 8, 1, 1), stream=s), lambda s: P.filter_tap_copy(f(8, 8, 1, 1), stream=s),
+             lambda s: P.nchw_to_nchwc(f(1, 8, 4, 4), 8, stream=s), lambda s: P.nchwc_to_nchw(f(1, 1, 4, 4, 8), 8, stream=s),
+             lambda s: P.kcrs_to_kcrsck(f(8, 8, 1, 1), 8, 1, stream=s),
+             lambda s: P.bnorm_fwd(f(1, 8, 4, 4), f(8), f(8), f(8), f(8), stream=s)]
+    for i, call in enumerate(calls):
+        with pytest.raises(Allocated) as e:
+            call("side")
+        assert e.value.args == ("side",), i

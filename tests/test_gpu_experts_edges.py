@@ -82,3 +82,26 @@ def test_calls_on_another_stream_leave_the_current_streams_memory_alone(P):
         at = t.untyped_storage().data_ptr()
         assert not any(a < at + t.untyped_storage().nbytes() and at < a + n for a, n in freed), name
         assert torch.equal(t.reshape(-1).view(torch.uint8), values[name].reshape(-1).view(torch.uint8)), name
+
+
+def test_convolutions_on_another_stream_leave_the_current_streams_memory_alone(P):
+    import torch
+    g = gen(5)
+    x, w = randn(g, 2, 64, 14, 14), randn(g, 64, 64, 3, 3)
+    xh, wh = x.bfloat16(), w.bfloat16()
+    side = torch.cuda.Stream()
+
+    def run(stream):
+        return [P.conv2d_fwd(x, w, pad=1, stream=stream), P.conv2d_fwd_bf16(xh, wh, pad=1, stream=stream), P.filter_tap_copy(w, stream=stream),
+                P.nchw_to_nchwc(x, 8, stream=stream)]
+    want = run(None)
+    torch.cuda.synchronize()
+    values = [t.clone() for t in want]
+    freed = [(t.untyped_storage().data_ptr(), t.untyped_storage().nbytes()) for t in want]
+    del want
+    got = run(side)
+    side.synchronize()
+    for t, v in zip(got, values):
+        at = t.untyped_storage().data_ptr()
+        assert not any(a < at + t.untyped_storage().nbytes() and at < a + n for a, n in freed)
+        assert torch.equal(t, v)
