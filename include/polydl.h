@@ -319,7 +319,8 @@ int polydl_grouped_gemm_dw_bf16(int E, int M, int N, int K, const int32_t *offse
  *   scales [E][NT][KT*128/group][16] bfloat16, 8-byte aligned;   zeros the same shape, uint8 0 .. 15, or NULL: 8.
  * Rows past N and inputs past K may hold any code; scales there must be finite.
  * polydl_w4_pack_bf16 writes it from w [E][N][K]: without zeros scale = max|w|/7 and codes 1 .. 15, with zeros scale =
- * (max(w,0) - min(w,0))/15; scales rounded to bfloat16 before the codes are found, codes rounded to nearest. */
+ * (max(w,0) - min(w,0))/15; scales rounded to bfloat16 before the codes are found, codes rounded to nearest.  The scale of a group with a NaN or
+ * an infinity is NaN, and so is every output of its row. */
 int polydl_w4_pack_bf16(int E, int N, int K, int group, const uint16_t *w, uint8_t *q, uint16_t *scales, uint8_t *zeros, void *stream);
 int polydl_w4_gemm_bf16(int E, int M, int N, int K, int group, const int32_t *offsets, const int32_t *rows, int x_rows, const uint16_t *x,
                         int64_t ldx, const uint8_t *q, const uint16_t *scales, const uint8_t *zeros, void *y, int64_t ldy, int out_type,

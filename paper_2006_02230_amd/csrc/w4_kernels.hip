@@ -1,5 +1,6 @@
 // The packing of weights into 4-bit codes, scales and zero points (few_rows.hip multiplies with them).
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include "experts.hpp"
 #include "internal.hpp"
 #include "lanes.hpp"
@@ -8,7 +9,8 @@ namespace polydl {
 
 // One wave a tile of 16 outputs and 128 inputs.  Without zero points: scale = max |w| / 7, q = round(w / scale) + 8, so
 // codes 1 to 15.  With: scale = (max(w, 0) - min(w, 0)) / 15, zero = round(-min / scale).  Scales are rounded to bfloat16
-// first and the codes found with the rounded scale.  Outputs past N have scale 0, inputs past K the code of a zero.
+// first and the codes found with the rounded scale.  Outputs past N have scale 0, inputs past K the code of a zero.  A NaN goes through
+// the extremes, an infinity becomes one: no code holds either, so the group's scale is NaN.
 __global__ __launch_bounds__(64) void w4_pack_kernel(int N, int K, int group, int tiles, int steps, const uint16_t *w, uint8_t *q,
                                                      uint16_t *scales, uint8_t *zeros)
 {
@@ -29,32 +31,33 @@ __global__ __launch_bounds__(64) void w4_pack_kernel(int N, int K, int group, in
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             v[i][j] = j & 1 ? bf16_hi(u[j >> 1]) : bf16_lo(u[j >> 1]);
-            lo[i] = fminf(lo[i], v[i][j]);
-            hi[i] = fmaxf(hi[i], v[i][j]);
+            lo[i] = __builtin_elementwise_minimum(lo[i], v[i][j]);
+            hi[i] = __builtin_elementwise_maximum(hi[i], v[i][j]);
         }
 #pragma unroll
         for (int x = 16; x < 64; x += 16) {
             if (x == 48) continue;
-            lo[i] = fminf(lo[i], __shfl_xor(lo[i], x));
-            hi[i] = fmaxf(hi[i], __shfl_xor(hi[i], x));
+            lo[i] = __builtin_elementwise_minimum(lo[i], __shfl_xor(lo[i], x));
+            hi[i] = __builtin_elementwise_maximum(hi[i], __shfl_xor(hi[i], x));
         }
     }
     if (words >= 2) {
 #pragma unroll
         for (int i = 0; i < 4; i += 2) {
-            lo[i] = lo[i + 1] = fminf(lo[i], lo[i + 1]);
-            hi[i] = hi[i + 1] = fmaxf(hi[i], hi[i + 1]);
+            lo[i] = lo[i + 1] = __builtin_elementwise_minimum(lo[i], lo[i + 1]);
+            hi[i] = hi[i + 1] = __builtin_elementwise_maximum(hi[i], hi[i + 1]);
         }
     }
     if (words == 4) {
-        lo[0] = lo[1] = lo[2] = lo[3] = fminf(lo[0], lo[2]);
-        hi[0] = hi[1] = hi[2] = hi[3] = fmaxf(hi[0], hi[2]);
+        lo[0] = lo[1] = lo[2] = lo[3] = __builtin_elementwise_minimum(lo[0], lo[2]);
+        hi[0] = hi[1] = hi[2] = hi[3] = __builtin_elementwise_maximum(hi[0], hi[2]);
     }
     lanes_u32x4 out;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+        const bool finite = hi[i] < INFINITY && lo[i] > -INFINITY;
         const float top = zeros ? (hi[i] - lo[i]) / 15.f : fmaxf(hi[i], -lo[i]) / 7.f;
-        const uint16_t bits = bf16_one(top);
+        const uint16_t bits = bf16_one(finite ? top : __builtin_nanf(""));
         const float scale = bf16_lo(bits), some = scale > 0.f ? scale : 1.f;
         const float zero = zeros ? fminf(fmaxf(rintf(-lo[i] / some), 0.f), 15.f) : 8.f;
         uint32_t word = 0u;

@@ -105,3 +105,30 @@ def test_convolutions_on_another_stream_leave_the_current_streams_memory_alone(P
         at = t.untyped_storage().data_ptr()
         assert not any(a < at + t.untyped_storage().nbytes() and at < a + n for a, n in freed)
         assert torch.equal(t, v)
+
+
+# ---- 4-bit weights ---------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("asymmetric", [False, True])
+@pytest.mark.parametrize("value", ["nan", "inf", "-inf"])
+def test_weights_that_no_code_holds_show(P, value, asymmetric, group):
+    import torch
+    E, N, K = 2, 37, 300
+    g = gen(group)
+    clean = randn(g, E, N, K).bfloat16()
+    w, x = clean.clone(), randn(g, 6, K).bfloat16()
+    broken = [(0, 0, 0), (0, 17, 131), (1, 36, K - 1), (1, 20, 64), (1, 20, 200)]
+    for at in broken:
+        w[at] = float(value)
+    a, b = P.w4_pack_bf16(clean, group, asymmetric), P.w4_pack_bf16(w, group, asymmetric)
+    scales = torch.zeros(b.scales.shape, dtype=torch.bool, device="cuda")
+    for e, n, k in broken:
+        scales[e, n // 16, k // group, n % 16] = True
+    assert torch.equal(torch.isnan(b.scales), scales) and torch.equal(b.scales[~scales], a.scales[~scales])
+    offsets = torch.tensor([0, 2, 6], dtype=torch.int32, device="cuda")
+    ya, yb = (P.w4_gemm_bf16(x, p.q, p.scales, N, group, zeros=p.zeros, offsets=offsets) for p in (a, b))
+    gone = torch.zeros(6, N, dtype=torch.bool, device="cuda")
+    for e, n, k in broken:
+        gone[[0, 1] if e == 0 else [2, 3, 4, 5], n] = True
+    assert torch.equal(torch.isnan(yb), gone) and torch.equal(yb[~gone], ya[~gone])
