@@ -56,7 +56,8 @@ __global__ __launch_bounds__(64) void w4_pack_kernel(int N, int K, int group, in
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const bool finite = hi[i] < INFINITY && lo[i] > -INFINITY;
-        const float top = zeros ? (hi[i] - lo[i]) / 15.f : fmaxf(hi[i], -lo[i]) / 7.f;
+        // (halves: the range may pass the largest float; halving is exact, so the quotient is the same)
+        const float top = zeros ? (0.5f * hi[i] - 0.5f * lo[i]) / 7.5f : fmaxf(hi[i], -lo[i]) / 7.f;
         const uint16_t bits = bf16_one(finite ? top : __builtin_nanf(""));
         const float scale = bf16_lo(bits), some = scale > 0.f ? scale : 1.f;
         const float zero = zeros ? fminf(fmaxf(rintf(-lo[i] / some), 0.f), 15.f) : 8.f;

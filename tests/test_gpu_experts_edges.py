@@ -132,3 +132,36 @@ def test_weights_that_no_code_holds_show(P, value, asymmetric, group):
     for e, n, k in broken:
         gone[[0, 1] if e == 0 else [2, 3, 4, 5], n] = True
     assert torch.equal(torch.isnan(yb), gone) and torch.equal(yb[~gone], ya[~gone])
+
+
+@pytest.mark.parametrize("group", [32, 64, 128])
+def test_weights_whose_range_passes_the_largest_float(P, group):
+    import torch
+    K = 256
+    w = randn(gen(group), 1, 16, K).bfloat16() * 1e37
+    w[0, :, 3], w[0, :, group - 1] = torch.finfo(torch.bfloat16).max, torch.finfo(torch.bfloat16).min
+    w[0, 1, group - 1] = 1.0
+    p = P.w4_pack_bf16(w, group, True)
+    scales = p.scales.double().cpu().numpy()
+    assert np.isfinite(scales).all()
+    back = ox.w4_weights(p.q.cpu().numpy(), p.scales.float().cpu().numpy(), p.zeros.cpu().numpy(), 16, K, group)
+    v = w.double().cpu().numpy()
+    parts = v.reshape(1, 16, -1, group)
+    scale = (np.maximum(parts.max(3), 0) - np.minimum(parts.min(3), 0)) / 15
+    # half a step, half a step more for the zero point, and the scale's rounding over 15 steps
+    bound = (scale * (1 + 2.0 ** -7) * (0.5 + 0.5 + 15 * 2.0 ** -8))[..., None]
+    assert (np.abs(back.reshape(parts.shape) - parts) <= bound).all()
+
+
+def test_scales_are_what_they_were(P):
+    # the range over 15 in 32 bits, rounded to bfloat16, small and large weights and the smallest ones there are
+    import torch
+    g = gen(1)
+    w = randn(g, 1, 64, 512) * torch.exp2(torch.randint(-140, 120, (1, 64, 1), generator=g, device="cuda").float())
+    w = w.bfloat16()
+    w[0, 0] = torch.randint(-2, 3, (512,), generator=g, device="cuda", dtype=torch.int16).abs().view(torch.bfloat16)
+    p = P.w4_pack_bf16(w, 128, True)
+    parts = w.float().reshape(64, 4, 128)
+    want = ((parts.amax(2).clamp(min=0) - parts.amin(2).clamp(max=0)) / 15).bfloat16()
+    got = p.scales.reshape(4, 4, 16).transpose(1, 2).reshape(64, 4)
+    assert torch.equal(got, want)
