@@ -19,7 +19,7 @@ bool too_long(int E, int M, int N, int K) { return E > kMaxLength || M > kMaxLen
 constexpr int64_t kMaxElements = 1ll << 60, kMaxRowStride = 1ll << 40;
 bool too_many(int64_t a, int64_t b, int64_t c) { return (__int128)a * b * c >= kMaxElements; }
 
-// hipErrorInvalidValue from a launcher here: no kernel holds the problem (a grid past 2^31)
+// hipErrorInvalidValue from a launcher here: no kernel holds the problem (2^31 - 2^20 workgroups)
 int launched_or_refused(hipError_t e) { return e == hipErrorInvalidValue ? POLYDL_ERR_UNSUPPORTED : launched(e); }
 
 }  // namespace

@@ -16,6 +16,7 @@
 // point gives exactly zero; otherwise both are rounded as sums of terms of up to 31 |x| are.
 #include <hip/hip_runtime.h>
 #include <type_traits>
+#include "blocks.hpp"
 #include "experts.hpp"
 #include "group_tiles.hpp"
 #include "internal.hpp"
@@ -151,7 +152,7 @@ __global__ __launch_bounds__(WAVES * 64) void few_rows_kernel(FewRowsProblem p, 
     GroupTile t;
     GroupTiles all;
     all.init(p.offsets, p.E, p.M, 16 * CT, col_tiles);
-    if (!all.find((int)blockIdx.x, &t)) return;
+    if (!all.find((int)block_number(), &t)) return;
     const int m0 = t.lo + t.m * 16 * CT, rows = min(16 * CT, t.hi - m0), n0 = t.n * RT;     // n0: in sixteens
     const int steps = t.e < p.E ? (p.K + W::kStep - 1) / W::kStep : 0;                      // slots behind the last group: zeros
 
@@ -245,10 +246,10 @@ static hipError_t few_rows_run(const FewRowsProblem &p, hipStream_t st)
 {
     const int64_t groups = p.M < p.E + 1 ? p.M : p.E + 1, col_tiles = ((p.N + 15) / 16 + RT - 1) / RT;
     const int64_t tiles = (p.M + groups * (16 * CT - 1)) / (16 * CT) * col_tiles;
-    if (tiles > 0x7fffffff) return hipErrorInvalidValue;
+    if (tiles > kMaxBlocks) return hipErrorInvalidValue;
     if (p.out_f32)
-        return launch_kernel((few_rows_kernel<W, RT, CT, WAVES, true>), dim3((unsigned)tiles), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
-    return launch_kernel((few_rows_kernel<W, RT, CT, WAVES, false>), dim3((unsigned)tiles), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
+        return launch_kernel((few_rows_kernel<W, RT, CT, WAVES, true>), many_blocks(tiles, WAVES * 64), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
+    return launch_kernel((few_rows_kernel<W, RT, CT, WAVES, false>), many_blocks(tiles, WAVES * 64), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
 }
 
 template <class W>

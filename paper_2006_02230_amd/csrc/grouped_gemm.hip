@@ -17,6 +17,7 @@
 #include <hip/hip_runtime.h>
 #include <atomic>
 #include <type_traits>
+#include "blocks.hpp"
 #include "experts.hpp"
 #include "gemm_core.hpp"
 #include "group_tiles.hpp"
@@ -327,8 +328,8 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             // the order of their lengths, the longest first (dW to bfloat16, groups' order / lengths' order: 16384 x 4096 x 2048 in 8 uneven groups 237 us /
             // 218, 32768 x 2048 x 2048 in 16 262 / 242; but 8192 x 1024 x 1024 in 32, where the order takes longer to find than it saves, 47 / 52)
             const int per = p.row_tiles * p.col_tiles, eighth = (per + 7) >> 3, at = id >> 3, turn = wave_value(at / eighth);
-            const int in = ((id + turn) & 7) * eighth + at - turn * eighth;
-            if (in >= per) return -1;
+            const int in = (((id & 7) + (turn & 7)) & 7) * eighth + at - turn * eighth;
+            if (in >= per || turn >= p.E) return -1;
             const int e = p.E <= kSorted && p.M >= 1024ll * p.E ? by_length(p.offsets, turn, p.E, p.M) : turn;
             const int m = wave_value(in / p.col_tiles), n = in - m * p.col_tiles;
             GroupRows g = group_rows(p.offsets, e, p.E, p.M);
@@ -583,7 +584,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
         }
     };
 
-    int id = (int)blockIdx.x;
+    int id = (int)block_number();
     GroupedOut now;
     int stages = find(id, now);
     if (stages < 0) return;
@@ -673,7 +674,7 @@ static hipError_t grouped_launch(const GroupedProblem &q, hipStream_t st)
         const int64_t groups = q.M < q.E + 1 ? q.M : q.E + 1;
         tiles = (q.M + groups * (BM - 1)) / BM * a.col_tiles;
     }
-    if (tiles > 0x7fff0000) return hipErrorInvalidValue;       // and a tile's number plus the workgroups is an int too
+    if (tiles > kMaxBlocks) return hipErrorInvalidValue;       // (a tile's number plus the workgroups is an int too)
     if (T::kLoops) {
         const int64_t fit = (int64_t)compute_units() * (160 * 1024 / T::kLds);
         if (tiles > fit) tiles = fit;
@@ -682,7 +683,7 @@ static hipError_t grouped_launch(const GroupedProblem &q, hipStream_t st)
         const hipError_t e = ask_lds<kernel>(T::kLds);
         if (e != hipSuccess) return e;
     }
-    return launch_kernel(kernel, dim3((unsigned)tiles), dim3(T::kThreads), T::kLds, st, a);
+    return launch_kernel(kernel, many_blocks(tiles, T::kThreads), dim3(T::kThreads), T::kLds, st, a);
 }
 
 template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA, bool GATHER, bool OUT_F32>

@@ -10,6 +10,7 @@
 // instructions of which 20 wait for one another.  16384 tokens, 128 experts, 8 choices: 7.6 us (13.6 with a wave to a token).
 #include <hip/hip_runtime.h>
 #include <math.h>
+#include "blocks.hpp"
 #include "experts.hpp"
 #include "internal.hpp"
 #include "lanes.hpp"
@@ -147,8 +148,9 @@ __global__ __launch_bounds__(1024) void route_choose_kernel(RouteArgs a)
     __shared__ uint32_t masks[2 * LANES * NV];
     __shared__ int count[ONE ? LANES * NV : 1], base[ONE ? LANES * NV + 1 : 1], part[16], ids[ONE ? kRouteTokens * kRouteMaxChoices : 1];
     const RouteProblem &p = a.p;
-    const int tid = threadIdx.x, l = tid % LANES;
-    const int t0 = blockIdx.x * kRouteTokens, nt = min(kRouteTokens, p.T - t0);
+    const int tid = threadIdx.x, l = tid % LANES, b = (int)block_number();
+    if (!ONE && b >= a.blocks) return;
+    const int t0 = b * kRouteTokens, nt = min(kRouteTokens, p.T - t0);
     for (int i = tid; i < 2 * p.E; i += 1024) masks[i] = 0u;
     __syncthreads();
     for (int t = tid / LANES; t < kRouteTokens; t += 1024 / LANES) {
@@ -173,9 +175,9 @@ __global__ __launch_bounds__(1024) void route_choose_kernel(RouteArgs a)
         route_place<1024>(p, ids, base, masks, 0, nt * p.k, tid);
         for (int s = base[p.E] + tid; s < nt * p.k; s += 1024) p.tokens[s] = -1;
     } else {
-        const int pad = blockIdx.x == gridDim.x - 1 ? a.pitch - a.blocks : 0;   // the bytes behind a row's end are zero too
+        const int pad = b == a.blocks - 1 ? a.pitch - a.blocks : 0;   // the bytes behind a row's end are zero too
         for (int e = tid; e < p.E; e += 1024) {
-            a.hist[(size_t)e * a.pitch + blockIdx.x] = (uint8_t)(__builtin_popcount(masks[2 * e]) + __builtin_popcount(masks[2 * e + 1]));
+            a.hist[(size_t)e * a.pitch + b] = (uint8_t)(__builtin_popcount(masks[2 * e]) + __builtin_popcount(masks[2 * e + 1]));
         }
         for (int i = tid; i < p.E * pad; i += 1024) {
             const int e = (int)((unsigned)i / (unsigned)pad);
@@ -211,7 +213,8 @@ __global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a)
     __shared__ int count[kRouteMaxExperts], base[kRouteMaxExperts + 1], ahead[kRouteMaxExperts], part[16];
     __shared__ int ids[kRouteTokens * kRouteMaxChoices];
     const RouteProblem &p = a.p;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = p.E, b = blockIdx.x;
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = p.E, b = (int)block_number();
+    if (b >= a.blocks) return;
     const int t0 = b * kRouteTokens, n = min(kRouteTokens, p.T - t0) * p.k;
     int held[kRouteTokens * kRouteMaxChoices / 1024];       // on their way while the counts are added up
 #pragma unroll
@@ -267,7 +270,7 @@ __global__ __launch_bounds__(1024) void route_place_kernel(RouteArgs a)
     }
     // slots that no choice took: behind the last expert's, dealt over the workgroups
     const int64_t M = (int64_t)p.T * p.k;
-    for (int64_t s = base[E] + (int64_t)b * 1024 + tid; s < M; s += (int64_t)gridDim.x * 1024) p.tokens[s] = -1;
+    for (int64_t s = base[E] + (int64_t)b * 1024 + tid; s < M; s += (int64_t)a.blocks * 1024) p.tokens[s] = -1;
     __syncthreads();
     for (int e = tid; e < E; e += 1024) base[e] += ahead[e];
     __syncthreads();
@@ -289,7 +292,7 @@ template <int LANES, int NV>
 static hipError_t route_choose(const RouteArgs &a, hipStream_t st)
 {
     if (a.blocks <= 1) return launch_kernel((route_choose_kernel<LANES, NV, true>), dim3(1), dim3(1024), 0, st, a);
-    return launch_kernel((route_choose_kernel<LANES, NV, false>), dim3((unsigned)a.blocks), dim3(1024), 0, st, a);
+    return launch_kernel((route_choose_kernel<LANES, NV, false>), many_blocks(a.blocks, 1024), dim3(1024), 0, st, a);
 }
 
 hipError_t route_launch(const RouteProblem &p, void *workspace, hipStream_t st)
@@ -312,10 +315,10 @@ hipError_t route_launch(const RouteProblem &p, void *workspace, hipStream_t st)
     hipError_t e = choose(a, st);
     if (e != hipSuccess || one) return e;
     if ((int64_t)a.blocks * a.pitch * p.E <= kRouteRereadBytes)
-        return launch_kernel(route_place_kernel<false>, dim3((unsigned)a.blocks), dim3(1024), 0, st, a);
+        return launch_kernel(route_place_kernel<false>, many_blocks(a.blocks, 1024), dim3(1024), 0, st, a);
     e = launch_kernel(route_scan_kernel, dim3((unsigned)((p.E + 3) / 4)), dim3(256), 0, st, a);
     if (e != hipSuccess) return e;
-    return launch_kernel(route_place_kernel<true>, dim3((unsigned)a.blocks), dim3(1024), 0, st, a);
+    return launch_kernel(route_place_kernel<true>, many_blocks(a.blocks, 1024), dim3(1024), 0, st, a);
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
@@ -327,7 +330,7 @@ __global__ __launch_bounds__(256) void route_bwd_kernel(int T, int E, int k, con
 {
     constexpr int kHeld = RouteRow<LANES>::kHeld;
     const int l = threadIdx.x % LANES, first = (threadIdx.x & 63) - l;
-    const int64_t t = (int64_t)blockIdx.x * (256 / LANES) + threadIdx.x / LANES;
+    const int64_t t = (int64_t)block_number() * (256 / LANES) + threadIdx.x / LANES;
     const bool here = t < T;
     int id[kHeld];
     float g[kHeld], w[kHeld], p[NV], own[NV];
@@ -397,7 +400,7 @@ template <int LANES, int NV>
 static hipError_t route_bwd(int T, int E, int k, const float *logits, const int32_t *ids, const float *weights, const float *dweights,
                             bool renorm, float *dlogits, hipStream_t st)
 {
-    const dim3 grid((unsigned)(((int64_t)T + 256 / LANES - 1) / (256 / LANES)));
+    const dim3 grid = many_blocks(((int64_t)T + 256 / LANES - 1) / (256 / LANES), 256);
     if (renorm)
         return launch_kernel((route_bwd_kernel<LANES, NV, true>), grid, dim3(256), 0, st, T, E, k, logits, ids, weights, dweights, dlogits);
     return launch_kernel((route_bwd_kernel<LANES, NV, false>), grid, dim3(256), 0, st, T, E, k, logits, ids, weights, dweights, dlogits);
@@ -425,7 +428,7 @@ __global__ __launch_bounds__(256) void combine_kernel(int T, int k, int M, int D
 {
     const int tl = units >= 256 ? 0 : (int)((unsigned)threadIdx.x / (unsigned)units);
     const int c = units >= 256 ? (int)(blockIdx.y * 256 + threadIdx.x) : (int)threadIdx.x - tl * units;
-    const int64_t t = (int64_t)blockIdx.x * per_block + tl;
+    const int64_t t = (int64_t)block_number() * per_block + tl;
     if (tl >= per_block || c >= units || t >= T) return;
     const int col = c * 8, n = min(8, D - col);
     float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
@@ -470,7 +473,7 @@ hipError_t combine_launch(int T, int k, int M, int D, const uint16_t *y, const i
                           bool out_f32, hipStream_t st)
 {
     const int units = (D + 7) / 8, per_block = units >= 256 ? 1 : 256 / units;
-    const dim3 grid((unsigned)((T + per_block - 1) / per_block), units >= 256 ? (unsigned)((units + 255) / 256) : 1u);
+    const dim3 grid = many_blocks(((int64_t)T + per_block - 1) / per_block, 256, units >= 256 ? (unsigned)((units + 255) / 256) : 1u);
     if (out_f32)
         return launch_kernel(combine_kernel<true>, grid, dim3(256), 0, st, T, k, M, D, units, per_block, y, slots, weights, out);
     return launch_kernel(combine_kernel<false>, grid, dim3(256), 0, st, T, k, M, D, units, per_block, y, slots, weights, out);
@@ -481,7 +484,7 @@ hipError_t combine_launch(int T, int k, int M, int D, const uint16_t *y, const i
 __global__ __launch_bounds__(256) void combine_bwd_kernel(int64_t MT, int k, int M, int D, const uint16_t *dout, const uint16_t *y,
                                                           const int32_t *slots, const float *weights, uint16_t *dy, float *dweights)
 {
-    const int64_t i = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int64_t i = (int64_t)block_number() * 4 + (threadIdx.x >> 6);
     const int lane = threadIdx.x & 63;
     if (i >= MT) return;
     const int s = slots[i];
@@ -519,7 +522,7 @@ hipError_t combine_bwd_launch(int T, int k, int M, int D, const uint16_t *dout, 
                               const float *weights, uint16_t *dy, float *dweights, hipStream_t st)
 {
     const int64_t MT = (int64_t)T * k;
-    return launch_kernel(combine_bwd_kernel, dim3((unsigned)((MT + 3) / 4)), dim3(256), 0, st, MT, k, M, D, dout, y, slots, weights, dy,
+    return launch_kernel(combine_bwd_kernel, many_blocks((MT + 3) / 4, 256), dim3(256), 0, st, MT, k, M, D, dout, y, slots, weights, dy,
                          dweights);
 }
 

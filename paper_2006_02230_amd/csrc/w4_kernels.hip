@@ -1,6 +1,7 @@
 // The packing of weights into 4-bit codes, scales and zero points (few_rows.hip multiplies with them).
 #include <hip/hip_runtime.h>
 #include <math.h>
+#include "blocks.hpp"
 #include "experts.hpp"
 #include "internal.hpp"
 #include "lanes.hpp"
@@ -11,14 +12,14 @@ namespace polydl {
 // codes 1 to 15.  With: scale = (max(w, 0) - min(w, 0)) / 15, zero = round(-min / scale).  Scales are rounded to bfloat16
 // first and the codes found with the rounded scale.  Outputs past N have scale 0, inputs past K the code of a zero.  A NaN goes through
 // the extremes, an infinity becomes one: no code holds either, so the group's scale is NaN.
-__global__ __launch_bounds__(64) void w4_pack_kernel(int N, int K, int group, int tiles, int steps, const uint16_t *w, uint8_t *q,
+__global__ __launch_bounds__(64) void w4_pack_kernel(int E, int N, int K, int group, int tiles, int steps, const uint16_t *w, uint8_t *q,
                                                      uint16_t *scales, uint8_t *zeros)
 {
     const int lane = threadIdx.x, row = lane & 15, quad = lane >> 4;
-    const int64_t id = blockIdx.x;
-    const int64_t tile = id / steps;
+    const int64_t id = block_number(), tile = id / steps;
     const int s = (int)(id - tile * steps);
     const int64_t e = tile / tiles;
+    if (e >= E) return;
     const int n = (int)(tile - e * tiles) * 16 + row;
     const int words = group / 32;
     float v[4][8], lo[4], hi[4];
@@ -81,8 +82,8 @@ hipError_t w4_pack_launch(int E, int N, int K, int group, const uint16_t *w, uin
 {
     const int tiles = (N + 15) / 16, steps = (K + 127) / 128;
     const int64_t all = (int64_t)E * tiles * steps;
-    if (all > 0x7fffffff) return hipErrorInvalidValue;
-    return launch_kernel(w4_pack_kernel, dim3((unsigned)all), dim3(64), 0, st, N, K, group, tiles, steps, w, q, scales, zeros);
+    if (all > kMaxBlocks) return hipErrorInvalidValue;
+    return launch_kernel(w4_pack_kernel, many_blocks(all, 64), dim3(64), 0, st, E, N, K, group, tiles, steps, w, q, scales, zeros);
 }
 
 }  // namespace polydl

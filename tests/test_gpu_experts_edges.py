@@ -165,3 +165,123 @@ def test_scales_are_what_they_were(P):
     want = ((parts.amax(2).clamp(min=0) - parts.amin(2).clamp(max=0)) / 15).bfloat16()
     got = p.scales.reshape(4, 4, 16).transpose(1, 2).reshape(64, 4)
     assert torch.equal(got, want)
+
+
+# ---- more threads than one axis of a grid holds (2^32) ------------------------------------------------------------------
+
+@pytest.fixture
+def room(P):
+    """Memory that earlier tests' tensors leave unused goes back before and after tests of large ones."""
+    import torch
+    torch.cuda.empty_cache()
+    yield
+    torch.cuda.empty_cache()
+
+
+def test_router_of_2_28_tokens(P, room):
+    # 1024 threads for 64 tokens in the choice and the plan
+    import torch
+    T = (1 << 28) + 70
+    x = randn(gen(1), T, 2)
+    x[-3] = -float("inf")
+    r = P.route(x, 1)
+    first = (x[:, 0] >= x[:, 1]) & (x[:, 0] != -float("inf"))
+    want = torch.where(first, 0, 1).int()
+    want[-3] = -1
+    assert torch.equal(r.ids[:, 0], want)
+    n0 = int(first.sum())
+    assert r.offsets.tolist() == [0, n0, T - 1]
+    at = torch.where(first, torch.cumsum(first, 0) - 1, n0 + torch.cumsum(want == 1, 0) - 1)    # by the tokens up to this one
+    at[-3] = -1
+    assert torch.equal(r.slots[:, 0], at.int())
+    tokens = torch.full((T,), -1, dtype=torch.int32, device="cuda")
+    there = want >= 0
+    tokens[at[there]] = there.nonzero()[:, 0].int()
+    assert torch.equal(r.tokens, tokens)
+    assert bool((r.weights[there] == 1).all()) and float(r.weights[-3]) == 0
+
+
+def test_router_gradient_of_2_28_tokens(P, room):
+    # 16 lanes a token
+    import torch
+    T = (1 << 28) + 9
+    x = randn(gen(2), T, 2)
+    ids = torch.zeros(T, 1, dtype=torch.int32, device="cuda")
+    d = torch.ones(T, 1, device="cuda")
+    got = torch.full((T, 2), 7.0, device="cuda")
+    P.route_bwd(x, ids, d, d, renorm=False, out=got)
+    assert not bool((got == 7).any())
+    for at in (0, 1 << 24, T - 5000):
+        p = torch.softmax(x[at:at + 5000].double(), 1)
+        want = p * (torch.tensor([1.0, 0.0], device="cuda") - p[:, :1])
+        # probabilities off by the roundings of a difference of up to 12, an exponential, a sum and a quotient, twice
+        assert float((got[at:at + 5000].double() - want).abs().max()) <= 2 * (2 * 12 + 8) * 2.0 ** -23
+
+
+def test_weighted_sum_of_2_24_long_rows(P, room):
+    # a workgroup of 256 for every token
+    import torch
+    T, D = (1 << 24) + 5, 1032
+    y = randn(gen(3), 3, D).bfloat16()
+    slots = (torch.arange(T, device="cuda") % 4 - 1).int().reshape(T, 1)                # -1, 0, 1, 2
+    out = P.combine_bf16(y, slots)
+    rows = torch.cat([torch.zeros_like(y[:1]), y])
+    for a in range(0, T, 1 << 20):
+        assert torch.equal(out[a:a + (1 << 20)], rows[slots[a:a + (1 << 20), 0].long() + 1]), a
+
+
+def test_gradient_of_the_weighted_sum_of_2_26_slots(P, room):
+    # a wave a slot
+    import torch
+    T, k, M, D = (1 << 21) + 1, 32, 40, 3
+    g = gen(4)
+    y, d, w = randn(g, M, D).bfloat16(), randn(g, T, D).bfloat16(), torch.ones(T, k, device="cuda")
+    slots = torch.full((T, k), -1, dtype=torch.int32, device="cuda")
+    places = [(0, 0, 5), (1 << 20, 31, 7), (T - 2, 3, 0), (T - 1, 0, 1), (T - 1, 31, 39)]
+    for t, j, s in places:
+        slots[t, j] = s
+    before = torch.full((M, D), 7.0, dtype=torch.bfloat16, device="cuda")
+    dy, dw = P.combine_bwd_bf16(d, y, slots, w, dy=before.clone())
+    want = before
+    for t, j, s in places:
+        want[s] = d[t]
+        assert abs(float(dw[t, j]) - float((d[t].double() * y[s].double()).sum())) <= 4 * 2.0 ** -23 * float((d[t].double() * y[s].double()).abs().sum())
+        dw[t, j] = 0
+    assert torch.equal(dy, want) and not bool(dw.any())
+
+
+def test_products_of_few_rows_with_2_29_columns(P, room):
+    # 256 threads for 32 columns
+    import torch
+    N = (1 << 29) + 40
+    w = randn(gen(5), 1, N, 1).bfloat16()
+    x = torch.full((1, 1), 0.7, device="cuda").bfloat16()
+    got = P.grouped_gemm_bf16(x, w, torch.tensor([0, 1], dtype=torch.int32, device="cuda"))
+    assert torch.equal(got[0], w[0, :, 0] * x[0])                     # one product, rounded once
+
+
+def test_gradient_of_the_weights_of_2_21_experts(P, room):
+    # eight workgroups of 256 for every expert
+    import torch
+    E = (1 << 21) + 3
+    offsets = torch.zeros(E + 1, dtype=torch.int32, device="cuda")
+    offsets[E // 2:], offsets[E] = 2, 5
+    dy, x = (randn(gen(s), 5, 1).bfloat16() for s in (6, 7))
+    got = torch.full((E, 1, 1), 7.0, device="cuda")
+    P.grouped_gemm_dw_bf16(dy, x, offsets, out=got)
+    for e, rows in ((E // 2 - 1, slice(0, 2)), (E - 1, slice(2, 5))):
+        terms = (dy[rows].double() * x[rows].double())
+        assert abs(float(got[e]) - float(terms.sum())) <= 34 * 2.0 ** -23 * float(terms.abs().sum())
+        got[e] = 0
+    assert not bool(got.any())
+
+
+def test_packing_of_2_26_tiles(P, room):
+    # 64 threads a tile
+    import torch
+    N = (1 << 30) + 48
+    w = randn(gen(8), N, 1).bfloat16()
+    p = P.w4_pack_bf16(w, 128)
+    for a in (0, 1 << 29, N - 64):
+        part = P.w4_pack_bf16(w[a:a + 64], 128)
+        assert torch.equal(p.q[:, a // 16:a // 16 + 4], part.q) and torch.equal(p.scales[:, a // 16:a // 16 + 4], part.scales)
