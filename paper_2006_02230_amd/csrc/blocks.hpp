@@ -1,5 +1,6 @@
-// Grids of any number of workgroups.  A launch holds fewer than 2^32 threads along one axis of its grid: more workgroups than that lie
-// along x and z, and block_number() is the workgroup's number among them.  The last row of z may go past the last one.
+// Grids of any number of workgroups.  A launch holds fewer than 2^32 threads along one axis of its grid; past that only what is left over
+// 2^32 runs, without an error (2^32 itself is one).  So more workgroups than that lie along x and z, and block_number() is the workgroup's
+// number among them.  The last row of z may go past the last one.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
