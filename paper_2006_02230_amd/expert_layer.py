@@ -13,30 +13,43 @@ from . import experts as X
 Gradients = collections.namedtuple("Gradients", "x router w1 w2")
 
 
+def _logits(x, router):
+    return B.sgemm(x, router, x.new_empty(x.shape[0], router.shape[1]), alpha=1.0, beta=0.0)
+
+
 class ExpertLayer:
     """out[t] = sum over the k chosen experts e of weight[t][e] * w2[e] relu(w1[e] x[t]), weights softmax(x[t] router) over the chosen.
 
-    router [D][E] float32, w1 [E][F][D] and w2 [E][D][F] bfloat16, x [T][D] bfloat16.  `forward` keeps what `backward` needs."""
+    router [D][E] float32, w1 [E][F][D] and w2 [E][D][F] bfloat16, x [T][D] bfloat16.  `forward` leaves what `backward` needs in `kept`;
+    with several forwards before their backwards, take it from there after each and give it to its backward."""
 
     def __init__(self, router, w1, w2, k):
         self.router, self.w1, self.w2, self.k = router, w1, w2, k
-        self.kept = None
+        self.kept, self.waiting = None, 0
 
-    def _logits(self, x):
-        return B.sgemm(x, self.router, x.new_empty(x.shape[0], self.router.shape[1]), alpha=1.0, beta=0.0)
-
-    def forward(self, x):
+    def forward(self, x, keep=True):
+        """out [T][D] bfloat16.  keep=False: an answer without a backward, of which nothing is kept."""
         xf = x.float()
-        logits = self._logits(xf)
+        logits = _logits(xf, self.router)
         r = X.route(logits, self.k)
         h = X.grouped_gemm_bf16(x, self.w1, r.offsets, rows=r.tokens, act="relu")
         y = X.grouped_gemm_bf16(h, self.w2, r.offsets)
-        self.kept = x, xf, logits, r, h, y
+        if keep:
+            self.kept, self.waiting = (x, xf, logits, r, h, y), self.waiting + 1
         return X.combine_bf16(y, r.slots, r.weights)
 
-    def backward(self, dout):
-        """Gradients(x bfloat16, router, w1, w2 float32) of the last forward, from the gradient of what it gave."""
-        x, xf, logits, r, h, y = self.kept
+    def backward(self, dout, kept=None):
+        """Gradients(x bfloat16, router, w1, w2 float32) of the forward that left `kept` (None: the only one since the last backward), from the
+        gradient of what it gave."""
+        if kept is None:
+            if self.kept is None:
+                raise RuntimeError("backward needs a forward that keeps")
+            if self.waiting > 1:
+                raise RuntimeError("%d forwards wait for their backward: give backward the one's `kept`, and keep=False to a forward without "
+                                   "a backward" % self.waiting)
+            kept = self.kept
+        self.waiting = max(self.waiting - 1, 0)
+        x, xf, logits, r, h, y = kept
         dy, dweights = X.combine_bwd_bf16(dout, y, r.slots, r.weights)
         dh = X.grouped_gemm_dx_bf16(dy, self.w2, r.offsets, h=h, act="relu")
         dw2 = X.grouped_gemm_dw_bf16(dy, h, r.offsets)
@@ -61,7 +74,7 @@ class CodedExpertLayer:
 
     def forward(self, x):
         l, (_, F, D) = self.layer, self.layer.w1.shape
-        r = X.route(l._logits(x.float()), l.k)
+        r = X.route(_logits(x.float(), l.router), l.k)
         h = X.w4_gemm_bf16(x, self.w1.q, self.w1.scales, F, self.group, zeros=self.w1.zeros, offsets=r.offsets, rows=r.tokens, act="relu")
         y = X.w4_gemm_bf16(h, self.w2.q, self.w2.scales, D, self.group, zeros=self.w2.zeros, offsets=r.offsets)
         return X.combine_bf16(y, r.slots, r.weights)
@@ -80,7 +93,7 @@ def main(steps=60, T=2048, D=256, F=512, E=16, k=2, seed=0):
     losses = []
     for step in range(steps):
         x = randn(T, D).bfloat16()
-        want = goal.forward(x).float()
+        want = goal.forward(x, keep=False).float()
         layer = ExpertLayer(master[0], master[1].bfloat16(), master[2].bfloat16(), k)
         error = layer.forward(x).float() - want
         losses.append(error.square().mean())
@@ -90,7 +103,7 @@ def main(steps=60, T=2048, D=256, F=512, E=16, k=2, seed=0):
             b.mul_(0.99).addcmul_(grad, grad, value=0.01)
             m.sub_(3e-3 * (a / (1 - 0.9 ** (step + 1))) / ((b / (1 - 0.99 ** (step + 1))).sqrt() + 1e-12))
     x = randn(T, D).bfloat16()
-    coded = (layer.coded(32, True).forward(x).float() - goal.forward(x).float()).square().mean()
+    coded = (layer.coded(32, True).forward(x).float() - goal.forward(x, keep=False).float()).square().mean()
     return float(losses[0]), float(losses[-1]), float(coded)
 
 

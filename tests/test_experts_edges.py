@@ -105,3 +105,86 @@ def test_every_call_allocates_for_its_stream(monkeypatch):
         with pytest.raises(Allocated) as e:
             call("side")
         assert e.value.args == ("side",), i
+
+
+@pytest.fixture
+def layer(monkeypatch):
+    """An ExpertLayer whose operators are their definitions in 64 bits on the CPU."""
+    import numpy as np
+    import torch
+
+    from oracle import experts as ox
+    from paper_2006_02230_amd import expert_layer as L
+    t, n = torch.tensor, lambda v: v.double().numpy()   # noqa: E731
+
+    def route(logits, k):
+        ids, w, offsets, tokens, slots = ox.route(n(logits), k, True)
+        return P.Route(t(ids), t(w), t(offsets), t(tokens), t(slots))
+
+    def groups(offsets):
+        return [slice(int(a), int(b)) for a, b in zip(offsets[:-1], offsets[1:])]
+
+    def forward(x, w, offsets, rows=None, act=None):
+        x = x if rows is None else x[rows]
+        return ox.act(torch.cat([x[g].double() @ w[e].double().T for e, g in enumerate(groups(offsets))]).numpy(), act)
+
+    def dx(dy, w, offsets, h=None, act=None, out_dtype=None):
+        d = torch.cat([dy[g].double() @ w[e].double() for e, g in enumerate(groups(offsets))])
+        return d if act is None else d * (h > 0)
+
+    def dw(dy, x, offsets, rows=None):
+        x = x if rows is None else x[rows]
+        return torch.stack([dy[g].double().T @ x[g].double() for g in groups(offsets)])
+
+    def combine(y, slots, weights=None, out_dtype=None):
+        return (y[slots] * (1.0 if weights is None else weights.unsqueeze(2))).sum(1)
+
+    def combine_bwd(dout, y, slots, weights):
+        dy = torch.empty_like(y)
+        dy[slots] = dout.double().unsqueeze(1) * weights.unsqueeze(2)
+        return dy, (dout.double().unsqueeze(1) * y[slots]).sum(2)
+
+    def sgemm(a, b, c, alpha=1.0, beta=1.0):
+        return c.copy_(beta * c + alpha * (a.double() @ b.double()) if beta else alpha * (a.double() @ b.double()))
+    for name, f in {"route": route, "grouped_gemm_bf16": lambda *a, **k: t(forward(*a, **k)), "grouped_gemm_dx_bf16": dx, "grouped_gemm_dw_bf16": dw,
+                    "combine_bf16": combine, "combine_bwd_bf16": combine_bwd,
+                    "route_bwd": lambda logits, ids, w, d: t(ox.route_bwd(n(logits), ids.numpy(), n(w), n(d), True)),
+                    "w4_pack_bf16": lambda w, *a: P.W4(w[:, :1, :1].clone(), w[:, :1, :1].clone(), None)}.items():
+        monkeypatch.setattr(L.X, name, f)
+    monkeypatch.setattr(L.B, "sgemm", sgemm)
+    r = np.random.RandomState(0)
+    make = lambda *s: t(r.randn(*s))   # noqa: E731
+    return L.ExpertLayer(make(6, 4), make(4, 5, 6), make(4, 6, 5), 2), make
+
+
+def same(a, b):
+    import torch
+    return all(torch.equal(p, q) for p, q in zip(a, b))
+
+
+def test_gradients_are_those_of_the_forward_they_belong_to(layer):
+    layer, make = layer
+    a, b, da, db = make(7, 6), make(7, 6), make(7, 6), make(7, 6)
+    with pytest.raises(RuntimeError):
+        layer.backward(da)
+    layer.forward(a)
+    want_a = layer.backward(da)
+    layer.forward(b)
+    want_b = layer.backward(db)
+    assert not same(want_a, want_b) and same(want_b, layer.backward(db))         # the last one's again
+    layer.forward(a)
+    kept_a = layer.kept
+    layer.forward(b)
+    with pytest.raises(RuntimeError):                                             # whose?
+        layer.backward(da)
+    kept_b = layer.kept
+    assert same(layer.backward(da, kept_a), want_a) and same(layer.backward(db, kept_b), want_b)
+    layer.forward(a)
+    layer.forward(b, keep=False)
+    assert same(layer.backward(da), want_a)
+
+
+def test_answers_keep_nothing(layer):
+    layer, make = layer
+    layer.forward(make(3, 6), keep=False)
+    assert layer.kept is None
