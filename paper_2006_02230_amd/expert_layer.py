@@ -69,12 +69,13 @@ class CodedExpertLayer:
     """An ExpertLayer that answers: weights in 4 bits, read once for every 64 rows of an expert."""
 
     def __init__(self, layer, group, asymmetric):
-        self.layer, self.group = layer, group
+        self.router, self.k, self.group = layer.router, layer.k, group
+        _, self.width, _ = layer.w1.shape
         self.w1, self.w2 = (X.w4_pack_bf16(w, group, asymmetric) for w in (layer.w1, layer.w2))
 
     def forward(self, x):
-        l, (_, F, D) = self.layer, self.layer.w1.shape
-        r = X.route(_logits(x.float(), l.router), l.k)
+        F, D = self.width, self.router.shape[0]
+        r = X.route(_logits(x.float(), self.router), self.k)
         h = X.w4_gemm_bf16(x, self.w1.q, self.w1.scales, F, self.group, zeros=self.w1.zeros, offsets=r.offsets, rows=r.tokens, act="relu")
         y = X.w4_gemm_bf16(h, self.w2.q, self.w2.scales, D, self.group, zeros=self.w2.zeros, offsets=r.offsets)
         return X.combine_bf16(y, r.slots, r.weights)

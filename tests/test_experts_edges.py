@@ -188,3 +188,15 @@ def test_answers_keep_nothing(layer):
     layer, make = layer
     layer.forward(make(3, 6), keep=False)
     assert layer.kept is None
+
+
+def test_weights_in_4_bits_take_the_others_place(layer):
+    import gc
+
+    import torch
+    layer, make = layer
+    coded, sizes = layer.coded(), {layer.w1.data_ptr(), layer.w2.data_ptr()}
+    held = [v for o in (coded, *vars(coded).values()) for v in gc.get_referents(o) if isinstance(v, torch.Tensor)]
+    held += [v for v in vars(coded).values() if isinstance(v, torch.Tensor)]
+    assert held and not any(v.data_ptr() in sizes for v in held)
+    assert not any(v is layer for v in vars(coded).values())
