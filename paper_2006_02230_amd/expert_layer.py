@@ -14,7 +14,8 @@ Gradients = collections.namedtuple("Gradients", "x router w1 w2")
 
 
 def _logits(x, router):
-    return B.sgemm(x, router, x.new_empty(x.shape[0], router.shape[1]), alpha=1.0, beta=0.0)
+    logits = x.new_empty(x.shape[0], router.shape[1])
+    return B.sgemm(x, router, logits, alpha=1.0, beta=0.0) if len(x) else logits           # sgemm has no empty matrices
 
 
 class ExpertLayer:
@@ -56,6 +57,8 @@ class ExpertLayer:
         dw1 = X.grouped_gemm_dw_bf16(dh, x, r.offsets, rows=r.tokens)
         dx = X.combine_bf16(X.grouped_gemm_dx_bf16(dh, self.w1, r.offsets, out_dtype=torch.bfloat16), r.slots, out_dtype=torch.float32)
         dlogits = X.route_bwd(logits, r.ids, r.weights, dweights)
+        if not len(x):
+            return Gradients(dx.bfloat16(), torch.zeros_like(self.router), dw1, dw2)
         drouter = B.sgemm(xf.t().contiguous(), dlogits, torch.empty_like(self.router), alpha=1.0, beta=0.0)
         B.sgemm(dlogits, self.router.t().contiguous(), dx)                     # added to what came through the experts
         return Gradients(dx.bfloat16(), drouter, dw1, dw2)

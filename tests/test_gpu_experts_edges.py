@@ -285,3 +285,18 @@ def test_packing_of_2_26_tiles(P, room):
     for a in (0, 1 << 29, N - 64):
         part = P.w4_pack_bf16(w[a:a + 64], 128)
         assert torch.equal(p.q[:, a // 16:a // 16 + 4], part.q) and torch.equal(p.scales[:, a // 16:a // 16 + 4], part.scales)
+
+
+# ---- the layer ----------------------------------------------------------------------------------------------------------
+
+def test_layer_without_tokens(P):
+    import torch
+    from paper_2006_02230_amd.expert_layer import ExpertLayer
+    g = gen(12)
+    layer = ExpertLayer(randn(g, 64, 4), randn(g, 4, 128, 64).bfloat16(), randn(g, 4, 64, 128).bfloat16(), 2)
+    x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    assert layer.forward(x).shape == (0, 64) and layer.coded().forward(x).shape == (0, 64)
+    grads = layer.backward(x)
+    assert grads.x.shape == (0, 64) and grads.x.dtype == torch.bfloat16
+    for got, like in ((grads.router, layer.router), (grads.w1, layer.w1), (grads.w2, layer.w2)):
+        assert got.shape == like.shape and got.dtype == torch.float32 and not bool(got.any())
