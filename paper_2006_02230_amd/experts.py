@@ -4,6 +4,9 @@ with 4-bit weights (same names as the C entry points, argument marshalling only)
 Rows sorted by expert, their offsets, `tokens` and `slots` are tensors on the device (`route` makes them); nothing here waits for the
 device.  Matrices may have any row stride; their columns are contiguous.
 
+The gradients are calls of their own (route_bwd, combine_bwd_bf16, grouped_gemm_dx_bf16, grouped_gemm_dw_bf16): results carry no graph, so while torch records one,
+the calls that have a gradient refuse arguments that require theirs.
+
 `stream` (None: torch's current stream) is where a call runs.  What it allocates is that stream's memory; as with any work on several streams, the
 caller makes `stream` wait for the arguments, keeps them until it has read them, and waits for it before using the results elsewhere."""
 import collections
@@ -44,6 +47,14 @@ def _device():
         return None
 
 
+def _no_graph(*tensors):
+    if torch.is_grad_enabled():
+        for t in tensors:
+            if t is not None and t.requires_grad:
+                raise RuntimeError("an argument requires its gradient, which would be lost: results carry no graph.  Call under torch.no_grad() or in "
+                                   "an autograd.Function, whose backward calls the operator's gradient")
+
+
 def _refuse(t, name, dtype, shape, dev):
     if not isinstance(t, torch.Tensor) or t.dtype != dtype:
         raise TypeError("%s must be a %s tensor" % (name, dtype))
@@ -81,6 +92,7 @@ def _type(dtype):
 
 def route(logits, k, renorm=True, stream=None):
     """polydl_route on float32 logits [T][E]: Route(ids [T][k], weights [T][k], offsets [E+1], tokens [T*k], slots [T][k])."""
+    _no_graph(logits)
     T, E = logits.shape
     src = _dense(logits, "logits", torch.float32, (T, E), _device())
     ids, slots, weights = _new((3, T, k), torch.int32, logits, stream).unbind(0)          # allocations take longer than views
@@ -106,6 +118,7 @@ def route_bwd(logits, ids, weights, dweights, renorm=True, out=None, stream=None
 
 def combine_bf16(y, slots, weights=None, out=None, out_dtype=torch.bfloat16, stream=None):
     """polydl_combine_bf16: [T][D] from y [M][D] (bfloat16), slots [T][k] and weights [T][k] (None: ones)."""
+    _no_graph(y, weights)
     (M, D), (T, k), dev = y.shape, slots.shape, _device()
     if out is None:
         out = _new((T, D), out_dtype, y, stream)
@@ -130,6 +143,7 @@ def combine_bwd_bf16(dout, y, slots, weights=None, dy=None, stream=None):
 
 def grouped_gemm_bf16(x, w, offsets, rows=None, act=None, out=None, out_dtype=torch.bfloat16, stream=None):
     """polydl_grouped_gemm_bf16: act(x[rows] @ w[e].T) for the rows of each group e; w [E][N][K], offsets [E+1], rows [M] or None."""
+    _no_graph(x, w)
     (E, N, K), x_rows, dev = w.shape, x.shape[0], _device()
     M = x_rows if rows is None else rows.shape[0]
     if out is None:
@@ -198,6 +212,7 @@ def w4_pack_bf16(w, group=128, asymmetric=False, stream=None):
 
 def w4_gemm_bf16(x, q, scales, N, group, zeros=None, offsets=None, rows=None, act=None, out=None, out_dtype=torch.bfloat16, stream=None):
     """polydl_w4_gemm_bf16: act(x[rows] @ w[e].T) with the packed 4-bit weights of w4_pack_bf16, [N][x.shape[1]] each."""
+    _no_graph(x, scales)
     E, (x_rows, K), dev = q.shape[0], x.shape, _device()
     M = x_rows if rows is None else rows.shape[0]
     codes, per_group = w4_shapes(E, N, K, group)

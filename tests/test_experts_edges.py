@@ -200,3 +200,28 @@ def test_weights_in_4_bits_take_the_others_place(layer):
     held += [v for v in vars(coded).values() if isinstance(v, torch.Tensor)]
     assert held and not any(v.data_ptr() in sizes for v in held)
     assert not any(v is layer for v in vars(coded).values())
+
+
+def test_arguments_whose_gradient_would_be_lost_are_refused():
+    import torch
+    z = lambda *s, d=torch.bfloat16: torch.zeros(*s, dtype=d)   # noqa: E731
+    f32, i32 = torch.float32, torch.int32
+    calls = [(P.route, (z(4, 8, d=f32),), (2,)), (P.combine_bf16, (z(4, 8), None), (z(2, 2, d=i32),)),
+             (P.combine_bf16, (z(4, 8), z(2, 2, d=f32)), (z(2, 2, d=i32),)), (P.grouped_gemm_bf16, (z(4, 8), z(2, 16, 8)), (z(3, d=i32),)),
+             (P.w4_gemm_bf16, (z(4, 8), z(1, 1, 4, 16)), (16, 32))]
+
+    def call(f, wants, rest):
+        if f is P.combine_bf16:
+            return f(wants[0], rest[0], wants[1])
+        if f is P.w4_gemm_bf16:
+            return f(wants[0], torch.zeros(1, 1, 1, 64, 16, dtype=torch.uint8), wants[1], *rest)
+        return f(*wants, *rest)
+    for f, wants, rest in calls:
+        for i, t in enumerate(wants):
+            if t is None:
+                continue
+            asks = [v if j != i else t.clone().requires_grad_() for j, v in enumerate(wants)]
+            with pytest.raises(RuntimeError, match="gradient"):
+                call(f, asks, rest)
+            with torch.no_grad(), pytest.raises(TypeError):            # host tensors
+                call(f, asks, rest)
