@@ -60,12 +60,12 @@ __device__ __forceinline__ gg_i32x4 gg_rsrc(uint64_t base, int64_t bytes)
 }
 // Sixteen bytes a lane into LDS at `lds` + 16 * lane; not waited for.  As assembly, because the compiler puts a wait for every such
 // load before each transposing LDS read, whichever buffer it reads (measured with stages of 32 at 16384 x 4096 x 2048: dX 1112
-// against 902, dW 865 against 512 TFLOP/s).  Nothing is written to a register; the waits are gg_wait()'s.  The wait states are those that a descriptor or m0 just written needs; nothing else
-// in these kernels uses m0.
+// against 902, dW 865 against 512 TFLOP/s).  No register is written; the waits are gg_wait()'s.  m0, where the
+// load's LDS address is, is an operand that the compiler sets and knows of; the wait states are those that a descriptor or m0 just written needs.
 __device__ __forceinline__ void gg_dma(gg_i32x4 rsrc, uint32_t lds, uint32_t off)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"s"(lds), "v"(off), "s"(rsrc) : "memory");
+    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(lds), "v"(off), "s"(rsrc) : "memory");
 #else
     (void)rsrc; (void)lds; (void)off;
 #endif

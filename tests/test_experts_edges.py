@@ -225,3 +225,14 @@ def test_arguments_whose_gradient_would_be_lost_are_refused():
                 call(f, asks, rest)
             with torch.no_grad(), pytest.raises(TypeError):            # host tensors
                 call(f, asks, rest)
+
+
+def test_assembly_leaves_no_register_that_the_compiler_does_not_know_of():
+    # registers named in the text of an assembly statement, rather than given as its operands
+    import glob
+    import os
+    import re
+    for path in glob.glob(os.path.join(os.path.dirname(P.__file__), "csrc", "*.h*")):
+        for text in re.findall(r"\basm\s*(?:volatile)?\s*\((\"[^;]*?);\n", open(path).read(), re.S):
+            code = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', text.split(":")[0]))
+            assert not re.search(r"\b(m0|vcc\w*|exec\w*|scc|[sva]\d+|[sva]\[\d+:\d+\])\b", code.replace("\\n", " ").replace("\\t", " ")), (path, code)
