@@ -47,12 +47,10 @@ def _device():
         return None
 
 
-def _no_graph(*tensors):
+def _no_graph():
     if torch.is_grad_enabled():
-        for t in tensors:
-            if t is not None and t.requires_grad:
-                raise RuntimeError("an argument requires its gradient, which would be lost: results carry no graph.  Call under torch.no_grad() or in "
-                                   "an autograd.Function, whose backward calls the operator's gradient")
+        raise RuntimeError("an argument requires its gradient, which would be lost: results carry no graph.  Call under torch.no_grad() or in an "
+                           "autograd.Function, whose backward calls the operator's gradient")
 
 
 def _refuse(t, name, dtype, shape, dev):
@@ -92,7 +90,8 @@ def _type(dtype):
 
 def route(logits, k, renorm=True, stream=None):
     """polydl_route on float32 logits [T][E]: Route(ids [T][k], weights [T][k], offsets [E+1], tokens [T*k], slots [T][k])."""
-    _no_graph(logits)
+    if logits.requires_grad:
+        _no_graph()
     T, E = logits.shape
     src = _dense(logits, "logits", torch.float32, (T, E), _device())
     ids, slots, weights = _new((3, T, k), torch.int32, logits, stream).unbind(0)          # allocations take longer than views
@@ -118,7 +117,8 @@ def route_bwd(logits, ids, weights, dweights, renorm=True, out=None, stream=None
 
 def combine_bf16(y, slots, weights=None, out=None, out_dtype=torch.bfloat16, stream=None):
     """polydl_combine_bf16: [T][D] from y [M][D] (bfloat16), slots [T][k] and weights [T][k] (None: ones)."""
-    _no_graph(y, weights)
+    if y.requires_grad or weights is not None and weights.requires_grad:
+        _no_graph()
     (M, D), (T, k), dev = y.shape, slots.shape, _device()
     if out is None:
         out = _new((T, D), out_dtype, y, stream)
@@ -143,7 +143,8 @@ def combine_bwd_bf16(dout, y, slots, weights=None, dy=None, stream=None):
 
 def grouped_gemm_bf16(x, w, offsets, rows=None, act=None, out=None, out_dtype=torch.bfloat16, stream=None):
     """polydl_grouped_gemm_bf16: act(x[rows] @ w[e].T) for the rows of each group e; w [E][N][K], offsets [E+1], rows [M] or None."""
-    _no_graph(x, w)
+    if x.requires_grad or w.requires_grad:
+        _no_graph()
     (E, N, K), x_rows, dev = w.shape, x.shape[0], _device()
     M = x_rows if rows is None else rows.shape[0]
     if out is None:
@@ -212,7 +213,8 @@ def w4_pack_bf16(w, group=128, asymmetric=False, stream=None):
 
 def w4_gemm_bf16(x, q, scales, N, group, zeros=None, offsets=None, rows=None, act=None, out=None, out_dtype=torch.bfloat16, stream=None):
     """polydl_w4_gemm_bf16: act(x[rows] @ w[e].T) with the packed 4-bit weights of w4_pack_bf16, [N][x.shape[1]] each."""
-    _no_graph(x, scales)
+    if x.requires_grad or scales.requires_grad:
+        _no_graph()
     E, (x_rows, K), dev = q.shape[0], x.shape, _device()
     M = x_rows if rows is None else rows.shape[0]
     codes, per_group = w4_shapes(E, N, K, group)
