@@ -263,7 +263,9 @@ static hipError_t few_rows_pick(const FewRowsProblem &p, hipStream_t st)
         const int64_t chunks = p.M < p.E ? p.M : p.E, tiles = chunks * ((p.N + 31) / 32), cus = compute_units();
         return tiles < cus ? few_rows_run<W, 1, 1, 8>(p, st) : tiles < 4 * cus ? few_rows_run<W, 2, 1, 8>(p, st) : few_rows_run<W, 2, 1, 4>(p, st);
     }
-    return rows <= 32 ? few_rows_run<W, 2, 2, 8>(p, st) : few_rows_run<W, 2, 4, 8>(p, st);
+    // (bfloat16 weights of more rows are the tiles')
+    if constexpr (std::is_same_v<W, WholeWeights>) return hipErrorInvalidValue;
+    else return rows <= 32 ? few_rows_run<W, 2, 2, 8>(p, st) : few_rows_run<W, 2, 4, 8>(p, st);
 }
 
 template <int GROUP>

@@ -105,15 +105,15 @@ __device__ __forceinline__ gg_f32x4 gg_mfma(lanes_u32x4 a, lanes_u32x4 b, gg_f32
 template <int R, int THREADS, bool RED_OUTER, bool DMA, bool GATHER>
 struct Operand {
     static constexpr int kAll = R * kStage / 8;                              // units of a stage
-    static constexpr int kUnits = kAll < THREADS ? 1 : kAll / THREADS;       // of a thread
+    static constexpr int kUnits = kAll / THREADS;                            // of a thread
     static constexpr int kRow = RED_OUTER ? R / 8 : kStage / 8;              // units of a row in LDS
     static constexpr int kBytes = kAll * 16;
-    static_assert((kAll % THREADS == 0 || kAll < THREADS) && THREADS % kRow == 0 && kAll % 64 == 0, "whole units, whole waves");
+    static_assert(kAll % THREADS == 0 && THREADS % kRow == 0, "whole units");
     static_assert(!RED_OUTER || R == 64 || R % 128 == 0, "the block permutation");
 
     static constexpr bool kIndexed = GATHER && RED_OUTER;        // the reduction's rows are read by index
     const char *base;                 // of the tile; GATHER: of the tensor (RED_OUTER: of the tile's columns in it)
-    int64_t ld, bytes;                // from row to row; from base to the end of what may be read
+    int64_t ld, bytes;                // from row to row; from base to the end of what may be read (RED_OUTER without GATHER: else offsets say it)
     int red, count;                   // length of the reduction; rows or columns of the tile that exist
     int length;                       // RED_OUTER: of a row in memory, columns of other tiles included
     const int32_t *rows;              // GATHER: of the tile's rows (innermost), of the reduction's (outermost)
@@ -137,7 +137,6 @@ struct Operand {
         return R == 64 ? ((kr >> 1) & 1) | ((kr >> 3) & 1) << 1 : (kr & 3) | ((kr >> 3) & 1) << 2;
     }
     static __device__ __forceinline__ int turn(int r) { return r & 7; }
-    static __device__ __forceinline__ bool mine(int tid) { return kAll >= THREADS || tid < kAll; }
     static __device__ __forceinline__ int lds_row(int tid, int i) { return tid / kRow + i * (THREADS / kRow); }
     // which unit of its row the thread's unit i holds
     static __device__ __forceinline__ int unit_of(int tid, int i)
@@ -204,7 +203,6 @@ struct Operand {
     }
     __device__ __forceinline__ void unit(int s, int i, char *lds, int tid)
     {
-        if (!mine(tid)) return;
         const int k0 = s * kStage;
         if constexpr (DMA) {
             uint32_t o = off[i];
@@ -224,7 +222,6 @@ struct Operand {
     __device__ __forceinline__ void commit(char *lds, int tid)
     {
         if constexpr (!DMA) {
-            if (!mine(tid)) return;
 #pragma unroll
             for (int i = 0; i < kUnits; ++i) *reinterpret_cast<lanes_u32x4 *>(lds + (i * THREADS + tid) * 16) = held[i];
         }
@@ -309,10 +306,8 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             const bool gathered = FORM == GROUPED_FWD && p.rows;
             A.rows = gathered ? p.rows + m0 : nullptr;
             A.base = gathered ? p.a : p.a + m0 * p.lda;
-            A.bytes = (int64_t)(gathered ? p.src_rows - 1 : out.rows - 1) * p.lda + (int64_t)p.red * 2;
             if constexpr (FORM == GROUPED_FWD) {
                 B.base = p.b + ((int64_t)e * p.cols + n0) * p.ldb;
-                B.bytes = (int64_t)(out.cols - 1) * p.ldb + (int64_t)p.red * 2;
             } else {
                 B.base = p.b + (int64_t)e * p.red * p.ldb + (int64_t)n0 * 2;
                 B.bytes = (int64_t)(p.red - 1) * p.ldb + (int64_t)out.cols * 2;
@@ -342,7 +337,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             A.bytes = (int64_t)(red - 1) * p.lda + (int64_t)out.rows * 2;
             B.rows = p.rows ? p.rows + g.lo : nullptr;
             B.base = p.b + (p.rows ? 0 : g.lo * p.ldb) + (int64_t)n * BN * 2;
-            B.bytes = (int64_t)((p.rows ? p.src_rows : red) - 1) * p.ldb + (int64_t)out.cols * 2;
+            B.bytes = (int64_t)(red - 1) * p.ldb + (int64_t)out.cols * 2;
             A.red = B.red = red;
             out.c0 = ((int64_t)e * p.out_rows + (int64_t)m * BM) * p.ldc + (int64_t)n * BN;
             out.h0 = 0;
@@ -377,9 +372,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
     // waits until this wave's loads are down to those of BEHIND stages (DMA) or to none, then for the other waves
     const auto land = [&](auto behind) {
         constexpr int kBehind = T::kDma ? decltype(behind)::value : 0;
-        if (T::A::mine(tid) && T::B::mine(tid)) gg_wait<kBehind * kLoads>();
-        else if (T::B::mine(tid)) gg_wait<kBehind * T::B::kUnits>();
-        else gg_wait<0>();
+        gg_wait<kBehind * kLoads>();
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_sched_barrier(0);
     };
@@ -522,7 +515,7 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
                     if constexpr (OUT_F32) {
                         Floats4 *at = reinterpret_cast<Floats4 *>(c);
                         gg_f32x4 f = __builtin_bit_cast(gg_f32x4, v);
-                        if (p.accumulate) f += *at;
+                        if (FORM == GROUPED_DW && p.accumulate) f += *at;
                         if constexpr (PAST) __builtin_nontemporal_store(f, at);
                         else *at = f;
                     } else {
@@ -549,12 +542,12 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
                     float *c = static_cast<float *>(p.c) + at;
                     gg_f32x4 f = __builtin_bit_cast(gg_f32x4, v);
                     if (left >= 4) {
-                        if (p.accumulate) f += *reinterpret_cast<const Floats4 *>(c);
+                        if (FORM == GROUPED_DW && p.accumulate) f += *reinterpret_cast<const Floats4 *>(c);
                         *reinterpret_cast<Floats4 *>(c) = f;
                     } else {
 #pragma unroll
                         for (int q = 0; q < 3; ++q)
-                            if (q < left) c[q] = p.accumulate ? c[q] + f[q] : f[q];
+                            if (q < left) c[q] = FORM == GROUPED_DW && p.accumulate ? c[q] + f[q] : f[q];
                     }
                 } else {
                     uint16_t *c = static_cast<uint16_t *>(p.c) + at;

@@ -47,10 +47,6 @@ __device__ __forceinline__ uint64_t wave_value(uint64_t x)
     return (uint64_t)(uint32_t)wave_value((int)(uint32_t)(x >> 32)) << 32 | (uint32_t)wave_value((int)(uint32_t)x);
 }
 __device__ __forceinline__ int lane_of(int x, int lane) { return __builtin_amdgcn_readlane(x, lane); }
-__device__ __forceinline__ float lane_of(float x, int lane)
-{
-    return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
-}
 
 // Over LANES neighbouring lanes, 16 (a row: four rotations) or 64, the result in all of them.
 #define POLYDL_ROW_STEPS(STEP) STEP(0x128) STEP(0x124) STEP(0x122) STEP(0x121)
