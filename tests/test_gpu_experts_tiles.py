@@ -1,6 +1,9 @@
 """The products grouped by expert in every kind of tile: each case names the tile that the library's rule takes for it, by a copy of that rule,
 so that no kernel goes untested.  Groups are uneven: empty ones, of one row, ending inside tiles, with slots behind the last."""
+import numpy as np
 import pytest
+
+from oracle import experts as ox
 
 pytestmark = pytest.mark.gpu
 
@@ -123,7 +126,7 @@ EIGHT = (2500, 0, 1900, 1, 2049, 3000, 2300, 2050)                              
 FORWARD = [
     (256, SIXTEEN, 33, 2056, 264), (256, (3000, 1, 0, 5500), 7, 4104, 72), (128, SIXTEEN, 33, 1032, 136), (64, (65, 0, 100, 31), 5, 200, 136),
     ("reg 128", EIGHT, 9, 2047, 131), ("reg 64", (65, 0, 100, 31), 5, 203, 133), (256, tuple(150 + 13 * i for i in range(70)), 11, 2048, 72),
-    (64, tuple(i % 41 for i in range(150)), 11, 136, 72), ("few", (20, 0, 3, 40, 1, 0, 0, 5), 3, 200, 136),
+    (64, tuple(i % 41 for i in range(150)), 11, 136, 72), (256, (30000, 19000, 159), 0, 2056, 64), ("few", (20, 0, 3, 40, 1, 0, 0, 5), 3, 200, 136),
 ]
 
 
@@ -288,3 +291,85 @@ def test_offsets_that_are_no_plan(P, M, N, K, reg, sides):
             assert torch.equal(z, P.w4_gemm_bf16(x, q.q, q.scales, N, 32, zeros=q.zeros, offsets=good, out_dtype=dtype))
             assert torch.equal(dx, P.grouped_gemm_dx_bf16(dy, w, good, out_dtype=dtype))
             assert torch.equal(dw, P.grouped_gemm_dw_bf16(dy, x, good, out_dtype=dtype))
+
+
+# ---- few rows ----------------------------------------------------------------------------------------------------------
+
+def few_tile(E, M, N):
+    """Sixteens of outputs and of rows that a workgroup of the few-rows kernel takes, and its waves."""
+    rows, tiles = up(M, E), min(M, E) * up(N, 32)
+    if rows <= 16:
+        return (1, 1, 8) if tiles < CUS else (2, 1, 8) if tiles < 4 * CUS else (2, 1, 4)
+    return (2, 2, 8) if rows <= 32 else (2, 4, 8)
+
+
+# what few_tile says, rows of each group, slots behind the last one, N, K
+FEW = [
+    ((1, 1, 8), (3, 0, 17, 1), 2, 200, 300), ((2, 1, 8), (0, 1, 16, 17, 33, 2, 0, 5), 3, 1110, 300), ((2, 1, 4), (1, 0, 40, 16, 5, 17, 2, 3) * 2, 5, 2090, 260),
+    ((2, 2, 8), (70, 0, 16, 17, 1), 9, 130, 333), ((2, 4, 8), (200, 64, 0, 65, 1), 9, 130, 333),
+]
+
+
+@pytest.mark.parametrize("gather", [False, True])
+@pytest.mark.parametrize("case,kind", [(c, kind) for c in FEW for kind in ("bfloat16", "32", "64", "128", "32 zeros", "64 zeros", "128 zeros")
+                                       if c[0][1] == 1 or kind != "bfloat16"],           # bfloat16 weights of more rows are the tiles'
+                         ids=lambda v: v if isinstance(v, str) else "%dx%dx%d" % v[0])
+def test_few_rows(P, case, kind, gather):
+    import torch
+    shape, counts, tail, N, K = case
+    E = len(counts)
+    offsets, M = ragged(counts, tail)
+    assert few_tile(E, M, N) == shape and (kind != "bfloat16" or tile("fwd", E, M, N, K, True) == "few")
+    g = gen(M + N)
+    x, w = randn(g, max(1, M // 2) if gather else M, K).bfloat16(), (randn(g, E, N, K) * K ** -0.5).bfloat16()
+    rows = row_indices(M, x.shape[0], offsets[-1], 3) if gather else None
+    if not gather:
+        x[offsets[-1]:] = float("nan")
+    xs = gathered(x, rows) if gather else x.double()
+    if kind == "bfloat16":
+        weights, big = w.double(), w.double().abs()
+
+        def product(act, out):
+            P.grouped_gemm_bf16(x, w, ints(offsets), rows=rows, act=act, out=out)
+    else:
+        group = int(kind.split()[0])
+        q = P.w4_pack_bf16(w, group, "zeros" in kind)
+        codes, scales, zeros = q.q.cpu().numpy(), q.scales.float().cpu().numpy(), None if q.zeros is None else q.zeros.cpu().numpy()
+        weights = torch.tensor(ox.w4_weights(codes, scales, zeros, N, K, group), device="cuda")
+        # the sums are of (16 + q) x and (16 + zero) x, at most 31 scale |x| each
+        big = torch.tensor(ox.w4_weights(np.zeros_like(codes), scales, None, N, K, group), device="cuda").abs() * (62 / 8)
+
+        def product(act, out):
+            P.w4_gemm_bf16(x, q.q, q.scales, N, group, zeros=q.zeros, offsets=ints(offsets), rows=rows, act=act, out=out)
+    for act, dtype in ((None, torch.float32), ("relu", torch.bfloat16)):
+        out, whole = guarded((M, N), dtype, 3 if gather else 4)
+        product(act, out)
+        whole()
+        assert not bool(out[offsets[-1]:].any())
+        for e in range(E):
+            a, b = offsets[e], offsets[e + 1]
+            want = xs[a:b] @ weights[e].T
+            close(out[a:b], want if act is None else want.clamp(min=0), xs[a:b].abs() @ big[e].T, K, (e, act))
+
+
+# ---- router ------------------------------------------------------------------------------------------------------------
+
+@pytest.mark.parametrize("E", [16, 17, 32, 33, 64, 65, 128, 129, 256, 257, 512, 513, 1024])
+@pytest.mark.parametrize("T", [3, 64, 65, 500])
+def test_router_of_every_width(P, T, E):
+    # a kernel for every number of logits a lane holds, alone and with a plan of its own
+    import torch
+    g = gen(T + E)
+    k = min(E, 17)                                                     # more choices than lanes take a token at once
+    x, d = randn(g, T, E), randn(g, T, k)
+    x[T // 2, ::2] = -float("inf")
+    for renorm in (False, True):
+        r = P.route(x, k, renorm=renorm)
+        ids, w, offsets, tokens, slots = ox.route(x.cpu().numpy(), k, renorm)
+        for got, want in zip((r.ids, r.offsets, r.tokens, r.slots), (ids, offsets, tokens, slots)):
+            assert np.array_equal(got.cpu().numpy(), want)
+        # logits of at most 6: a difference, exponentials, a sum and a quotient
+        assert np.abs(r.weights.cpu().numpy() - w).max() <= (2 * 12 + 24 + E / 64) * 2.0 ** -23
+        got = P.route_bwd(x, r.ids, r.weights, d, renorm=renorm).cpu().numpy().astype(np.float64)
+        want = ox.route_bwd(x.cpu().numpy(), ids, r.weights.cpu().numpy().astype(np.float64), d.cpu().numpy().astype(np.float64), renorm)
+        assert np.abs(got - want).max() <= 2 * np.abs(d.cpu().numpy()).max() * (2 * 12 + 24 + E / 64 + 2 * k) * 2.0 ** -23
