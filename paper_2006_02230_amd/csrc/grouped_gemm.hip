@@ -372,8 +372,11 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
     // waits until this wave's loads are down to those of BEHIND stages (DMA) or to none, then for the other waves
     const auto land = [&](auto behind) {
         constexpr int kBehind = T::kDma ? decltype(behind)::value : 0;
+        // (the builtins say nothing of memory: without the statements around them the compiler may move reads and writes of LDS past the barrier)
+        asm volatile("" ::: "memory");
         gg_wait<kBehind * kLoads>();
         __builtin_amdgcn_s_barrier();
+        asm volatile("" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
     };
     // the n-th operand of a stage: the columns', then the rows'

@@ -236,3 +236,15 @@ def test_assembly_leaves_no_register_that_the_compiler_does_not_know_of():
         for text in re.findall(r"\basm\s*(?:volatile)?\s*\((\"[^;]*?);\n", open(path).read(), re.S):
             code = "".join(re.findall(r'"((?:[^"\\]|\\.)*)"', text.split(":")[0]))
             assert not re.search(r"\b(m0|vcc\w*|exec\w*|scc|[sva]\d+|[sva]\[\d+:\d+\])\b", code.replace("\\n", " ").replace("\\t", " ")), (path, code)
+
+
+def test_barriers_order_memory_for_the_compiler_too():
+    # the bare builtin of a barrier orders the waves, not what the compiler does with reads and writes around it
+    import glob
+    import os
+    import re
+    for path in glob.glob(os.path.join(os.path.dirname(P.__file__), "csrc", "*.h*")):
+        text = open(path).read()
+        bare = len(re.findall(r"__builtin_amdgcn_s_barrier\(\)", text))
+        clobber = r'asm volatile\("" ::: "memory"\);\s*'
+        assert bare == len(re.findall(clobber + r"(?:gg_wait<[^;]*;\s*)?__builtin_amdgcn_s_barrier\(\);\s*" + clobber, text)), path
