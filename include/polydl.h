@@ -311,7 +311,8 @@ int polydl_grouped_gemm_dw_bf16(int E, int M, int N, int K, const int32_t *offse
 
 /* Products with 4-bit weights, for few rows: y[s][n] = act(sum_g scale[n][g] * sum_{k in g} (q[n][k] - zero[n][g]) * x[r(s)][k]),
  * groups g of `group` (32, 64 or 128) inputs; grouping by expert and rows as above, offsets NULL with E = 1: all rows.
- * Right for any number of rows; the weights are read once for every 64 rows of a group.  The codes enter the matrix cores as 16 + q and the 16
+ * Right for any number of rows; the weights are read once for every 16 rows of a group where M/E is at most 16, for every 32 where it is
+ * at most 32, else for every 64.  The codes enter the matrix cores as 16 + q and the 16
  * leaves again in float32: a row that holds an infinity or NaN, or whose sums of 31 |x| overflow, gives NaN or infinities.
  * The layout, KT = ceil(K/128) steps and NT = ceil(N/16) tiles:
  *   q      [E][NT][KT][64][16] bytes, 16-byte aligned: lane l of step s holds row 16*tile + l%16; nibble p (0 = low bits) of its i-th

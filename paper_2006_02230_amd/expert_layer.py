@@ -69,7 +69,7 @@ class ExpertLayer:
 
 
 class CodedExpertLayer:
-    """An ExpertLayer that answers: weights in 4 bits, read once for every 64 rows of an expert."""
+    """An ExpertLayer that answers: weights in 4 bits, read once for every 16, 32 or 64 rows of an expert, by the experts' mean."""
 
     def __init__(self, layer, group, asymmetric):
         self.router, self.k, self.group = layer.router, layer.k, group
