@@ -300,3 +300,27 @@ def test_layer_without_tokens(P):
     assert grads.x.shape == (0, 64) and grads.x.dtype == torch.bfloat16
     for got, like in ((grads.router, layer.router), (grads.w1, layer.w1), (grads.w2, layer.w2)):
         assert got.shape == like.shape and got.dtype == torch.float32 and not bool(got.any())
+
+
+def test_another_stream_inside_a_captured_graph(P):
+    import torch
+    g = gen(13)
+    x, w, logits = randn(g, 300, 128).bfloat16(), randn(g, 8, 192, 128).bfloat16(), randn(g, 300, 8)
+    torch.cuda.synchronize()
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        main = torch.cuda.current_stream()
+        side.wait_stream(main)
+        r = P.route(logits, 2, stream=side)
+        y = P.grouped_gemm_bf16(x, w, r.offsets, rows=r.tokens, stream=side)
+        main.wait_stream(side)
+        out = P.combine_bf16(y, r.slots, r.weights)
+        del r, y
+    for seed in range(3):
+        logits.copy_(randn(gen(seed), 300, 8))
+        out.zero_()
+        graph.replay()
+        torch.cuda.synchronize()
+        r = P.route(logits, 2)
+        assert torch.equal(out, P.combine_bf16(P.grouped_gemm_bf16(x, w, r.offsets, rows=r.tokens), r.slots, r.weights)), seed
+        torch.cuda.synchronize()
