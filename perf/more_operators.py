@@ -267,7 +267,7 @@ def _quantise(x):
 def _pack(code):
     """The library's layout: two codes a byte, the lower half first, [...][16 KB]."""
     q = code.reshape(*code.shape[:-2], -1, 2)
-    return q[..., 0] | (q[..., 1] << 4)
+    return (q[..., 0] | (q[..., 1] << 4)).to(torch.uint8)
 
 
 _MAGNITUDES = (0.0, 0.5, 1.0, 1.5, 2.0, 3.0, 4.0, 6.0)
