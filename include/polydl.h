@@ -327,6 +327,75 @@ int polydl_w4_gemm_bf16(int E, int M, int N, int K, int group, const int32_t *of
                         int64_t ldx, const uint8_t *q, const uint16_t *scales, const uint8_t *zeros, void *y, int64_t ldy, int out_type,
                         int act /* polydl_act */, void *stream);
 
+/* ---- around a layer of experts --------------------------------------------------------------------
+ * What a layer of experts needs before and beside it in a training step: the norm of its rows, a loss that keeps its experts evenly used,
+ * the norm of all gradients and their clipping; and products of matrices in microscaled 4-bit floating point for answers, of one token or of
+ * a whole prompt.  Conventions as in the section above: no entry point waits for the device or keeps memory, all may be captured, sums
+ * are float32 or more and in an order that does not depend on the run, each result is rounded once to nearest even.
+ * Host arrays (polydl_grad_norm, polydl_clip_grads) are read during the call. */
+
+/* Layer norm of the rows of x [T][D]: mean_t = sum_j x_tj / D, rstd_t = 1 / sqrt(sum_j (x_tj - mean_t)^2 / D + eps),
+ * y_tj = (x_tj - mean_t) * rstd_t * gamma_j + beta_j.  x of x_type, y of y_type (polydl_type), gamma and beta D floats or NULL (ones, zeros).
+ * mean and rstd (T floats each) are what the gradient needs; each may be NULL.  eps >= 0.  A row of equal values with eps = 0 has an
+ * infinite rstd, and NaN where the formula has 0 * infinity.
+ * polydl_layernorm_bwd: from dy [T][D] (dy_type), with h = (x - mean) * rstd and g = dy * gamma,
+ *   dx_tj = rstd_t * (g_tj - sum_i g_ti / D - h_tj * sum_i g_ti h_ti / D), of x_type;
+ *   dgamma_j = sum_t dy_tj h_tj, dbeta_j = sum_t dy_tj, float32; accumulate != 0 adds to what they hold.
+ * Each of dx, dgamma and dbeta may be NULL and is not formed then.  workspace: polydl_layernorm_bwd_workspace_bytes(T, D) bytes, 4-byte
+ * aligned, contents undefined afterwards; not looked at where neither dgamma nor dbeta is asked for.  T = 0 gives dgamma and dbeta of zeros.
+ * D <= 2^24.  Rows (ldx, ldy, lddy, lddx elements apart) may be longer than D. */
+int polydl_layernorm_fwd(int T, int D, const void *x, int64_t ldx, int x_type, const float *gamma, const float *beta, float eps, void *y,
+                         int64_t ldy, int y_type, float *mean, float *rstd, void *stream);
+size_t polydl_layernorm_bwd_workspace_bytes(int T, int D);
+int polydl_layernorm_bwd(int T, int D, const void *dy, int64_t lddy, int dy_type, const void *x, int64_t ldx, int x_type, const float *mean,
+                         const float *rstd, const float *gamma, void *dx, int64_t lddx, float *dgamma, float *dbeta, int accumulate,
+                         void *workspace, size_t workspace_bytes, void *stream);
+
+/* Balance loss of a router.  logits [T][E] float32 and the choices ids [T][k] as polydl_route gives them.  p_t = softmax(logits[t]) (zeros for
+ * a row whose logits are all -infinity), rows = the rows that are not; counts_e = how many ids are e (ids outside [0, E) are none);
+ * shares_e = sum_t p_te / rows; with f_e = counts_e / sum_i counts_i,
+ *   loss = E * sum_e f_e * shares_e,
+ * 1 where every expert is chosen as often and as probable as the others.  No rows or no choices: 0 in their place.  A NaN or +infinity among
+ * the logits makes shares and loss NaN.  loss 1, counts E, shares E values, rows 1 value.
+ * workspace: polydl_balance_workspace_bytes(T, E) bytes (0 for few tokens; 4-byte aligned, contents undefined afterwards).
+ * E <= 1024, k <= 32, T*k < 2^31.  T = 0 gives zeros.
+ * polydl_balance_bwd: dlogits_te = coefficient * dloss * E / rows * p_te * (f_e - sum_i f_i p_ti), the choices taken as constant; dloss one
+ * float in device memory or NULL (1); counts and rows may be sums over several batches or devices.  accumulate != 0 adds to dlogits. */
+size_t polydl_balance_workspace_bytes(int T, int E);
+int polydl_balance(int T, int E, int k, const float *logits, const int32_t *ids, float *loss, int32_t *counts, float *shares, int32_t *rows,
+                   void *workspace, size_t workspace_bytes, void *stream);
+int polydl_balance_bwd(int T, int E, const float *logits, const int32_t *counts, const int32_t *rows, float coefficient, const float *dloss,
+                       float *dlogits, int accumulate, void *stream);
+
+/* Gradient norm.  n tensors of counts[i] values of types[i] (polydl_type) at grads[i], each dense; grads, counts and types are host arrays.
+ * polydl_grad_norm: *norm = sqrt of the sum of all squares, summed in 64 bits, so that no square overflows; 0 without values.
+ * polydl_clip_grads: and out[i] = grads[i] * min(1, max_norm / norm), of types[i]; out NULL: in place.  A norm that is not finite
+ * (an infinity or NaN among the values) changes no value, nor does one of max_norm or less: in place nothing is written then.  *norm is
+ * the norm before, and tells.  max_norm >= 0.  A tensor that is written must not overlap another one, read or written, except its own grads[i]
+ * exactly (POLYDL_ERR_UNSUPPORTED): a tensor that is listed twice would be scaled twice.  Empty tensors may be NULL.
+ * workspace: polydl_clip_workspace_bytes(n, counts) bytes, 8-byte aligned, contents undefined afterwards. */
+size_t polydl_clip_workspace_bytes(int n, const int64_t *counts);
+int polydl_grad_norm(int n, const void *const *grads, const int64_t *counts, const int *types, float *norm, void *workspace,
+                     size_t workspace_bytes, void *stream);
+int polydl_clip_grads(int n, const void *const *grads, const int64_t *counts, const int *types, double max_norm, void *const *out,
+                      float *norm, void *workspace, size_t workspace_bytes, void *stream);
+
+/* Microscaled 4-bit floating point.  A row of K values is held in KB = 4 * ceil(K / 128) blocks of 32: a scale 2^(b - 127), b a byte (255: NaN),
+ * and 32 codes of 4 bits, a sign and 0, 1/2, 1, 3/2, 2, 3, 4, 6 (the OCP microscaling formats' E8M0 and E2M1).
+ *   q [rows][16 * KB] bytes, 16-byte aligned: byte i of a row holds the codes of inputs 2 i (low half) and 2 i + 1;
+ *   scales [rows][KB] bytes, 4-byte aligned.  What lies behind K holds codes of zero and finite scales.
+ * polydl_mx4_quantise: b - 127 = floor(log2(max |v|)) - 2 of the block, at least -127 (-127 for zeros); codes nearest to v / scale, ties to the
+ * even one, above 6 as 6.  A block with a NaN or an infinity has scale 255.  x [rows][K] of x_type, ldx elements apart.
+ * polydl_mx4_dequantise: the values, rounded to type (exact for scales that polydl_mx4_quantise gives); a scale of 255 gives NaN.
+ * polydl_mx4_gemm: y[s][n] = act(sum_k x[r(s)][k] * w[e][n][k]) with x [x_rows] and w [E][N] both held so; groups, rows and results as
+ * polydl_grouped_gemm_bf16, offsets NULL with E = 1: all rows.  Products are formed by the matrix cores from the codes and summed in float32.
+ * A block of NaN gives NaN for its row (of x) or column (of w).  q and scales are dense. */
+int polydl_mx4_quantise(int64_t rows, int K, const void *x, int64_t ldx, int x_type, uint8_t *q, uint8_t *scales, void *stream);
+int polydl_mx4_dequantise(int64_t rows, int K, const uint8_t *q, const uint8_t *scales, void *y, int64_t ldy, int y_type, void *stream);
+int polydl_mx4_gemm(int E, int M, int N, int K, const int32_t *offsets, const int32_t *rows, int x_rows, const uint8_t *xq,
+                    const uint8_t *x_scales, const uint8_t *wq, const uint8_t *w_scales, void *y, int64_t ldy, int out_type,
+                    int act /* polydl_act */, void *stream);
+
 /* ---- the reuse model (sections "Working set size computation" and "Poly-ranking algorithm") ------
  * polydl_reuse_analyse (declared below, before polydl_reuse_bucket): the working sets of a small loop nest.
  * polydl_reuse_bucket: algorithm "Compute working set sizes w.r.t cache sizes": the n working set

@@ -15,6 +15,8 @@ from .binding import (lib, PolydlError, TileCfg, ACT, conv2d_fwd, conv2d_fwd_noa
                       RANKER_STATS, RANKER_PARAMS_PATH, reuse_analyse)
 from .experts import (Route, W4, combine_bf16, combine_bwd_bf16, grouped_gemm_bf16, grouped_gemm_dw_bf16, grouped_gemm_dx_bf16, route,
                       route_bwd, w4_gemm_bf16, w4_pack_bf16, w4_shapes)
+from .mx4 import Mx4, mx4_dequantise, mx4_gemm, mx4_quantise, mx4_shapes
+from .training import (Balance, Norm, NormGradients, balance, balance_bwd, clip_grads, grad_norm, layernorm_bwd, layernorm_fwd)
 
 __all__ = ["lib", "PolydlError", "TileCfg", "ACT", "conv2d_fwd", "conv2d_fwd_noalloc", "filter_tap_copy", "sgemm", "set_tile_override",
            "get_last_tile", "variants", "status_string", "LIB_PATH", "nchw_to_nchwc", "nchwc_to_nchw",
@@ -25,4 +27,6 @@ __all__ = ["lib", "PolydlError", "TileCfg", "ACT", "conv2d_fwd", "conv2d_fwd_noa
            "ranker_num_params", "ranker_set_params", "ranker_load", "ranker_stats_conv2d", "ranker_play",
            "ranker_tournament", "pick_conv2d_learned", "RANKER_STATS", "RANKER_PARAMS_PATH", "reuse_analyse",
            "Route", "W4", "combine_bf16", "combine_bwd_bf16", "grouped_gemm_bf16", "grouped_gemm_dw_bf16", "grouped_gemm_dx_bf16", "route",
-           "route_bwd", "w4_gemm_bf16", "w4_pack_bf16", "w4_shapes"]
+           "route_bwd", "w4_gemm_bf16", "w4_pack_bf16", "w4_shapes",
+           "Mx4", "mx4_dequantise", "mx4_gemm", "mx4_quantise", "mx4_shapes",
+           "Balance", "Norm", "NormGradients", "balance", "balance_bwd", "clip_grads", "grad_norm", "layernorm_bwd", "layernorm_fwd"]

@@ -1,0 +1,193 @@
+// The norm of many tensors taken as one vector, and their scaling to a largest norm.
+//
+// The tensors lie along one axis of chunks of kChunk values, none of which goes past a tensor's end; a launch takes the tensors that its arguments
+// have room for, so that no table has to reach the device first (a captured launch keeps it, too).  First the squares, added up in 64 bits by each
+// thread and workgroup; then the sum over the workgroups, the norm and the factor, by one workgroup; then the scaling.
+// Bound: HBM, every value read twice and written once; the 64-bit sums cost two instructions a value.
+#include <hip/hip_runtime.h>
+#include <math.h>
+#include "block.hpp"
+#include "blocks.hpp"
+#include "internal.hpp"
+#include "lanes.hpp"
+#include "values.hpp"
+
+namespace polydl {
+
+constexpr int kClipTensors = 120;       // of a launch: its arguments stay within 4 KB
+constexpr int kClipThreads = 256, kChunk = 8192;
+constexpr int kClipBlocks = 2048;       // of a launch, at most
+
+struct ClipTable {
+    const void *grad[kClipTensors];
+    void *out[kClipTensors];
+    int64_t count[kClipTensors];
+    int32_t first[kClipTensors + 1];    // chunk that tensor i begins with
+    uint32_t f32[(kClipTensors + 31) / 32];
+    int n;
+};
+static_assert(sizeof(ClipTable) <= 4000, "kernel arguments");
+
+// a chunk: which tensor, where it begins in it, and its length
+struct ClipChunk { int tensor; bool f32; int64_t at; int length; };
+__device__ __forceinline__ ClipChunk clip_chunk(const ClipTable &t, int chunk)
+{
+    int lo = 0, hi = t.n;               // first[lo] <= chunk < first[hi]
+    while (hi - lo > 1) {
+        const int mid = (lo + hi) >> 1;
+        if (t.first[mid] <= chunk) lo = mid;
+        else hi = mid;
+    }
+    const int64_t at = (int64_t)(chunk - t.first[lo]) * kChunk, left = t.count[lo] - at;
+    return {lo, (t.f32[lo >> 5] >> (lo & 31) & 1u) != 0u, at, (int)(left < kChunk ? left : kChunk)};
+}
+
+template <bool F32>
+__device__ __forceinline__ double clip_squares(const void *grad, int64_t at, int length)
+{
+    const auto *v = static_cast<const typename Values<F32>::T *>(grad) + at;
+    double sum = 0.0;
+#pragma unroll 4
+    for (int col = threadIdx.x * 8; col < length; col += kClipThreads * 8) {
+        float x[8];
+        Values<F32>::load(v, col, length, x);
+#pragma unroll
+        for (int q = 0; q < 8; ++q) sum += (double)x[q] * (double)x[q];
+    }
+    return sum;
+}
+
+// the sum over the workgroup in thread 0, in a fixed order
+template <int THREADS>
+__device__ __forceinline__ double clip_sum(double sum, double *part)
+{
+    part[threadIdx.x] = sum;
+    for (int n = THREADS / 2; n > 0; n >>= 1) {
+        __syncthreads();
+        if ((int)threadIdx.x < n) part[threadIdx.x] += part[threadIdx.x + n];
+    }
+    return part[0];
+}
+
+__global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(ClipTable t, double *parts)
+{
+    __shared__ double part[kClipThreads];
+    double sum = 0.0;
+    const int chunks = t.first[t.n];
+    for (int c = (int)blockIdx.x; c < chunks; c += (int)gridDim.x) {
+        const ClipChunk k = clip_chunk(t, c);
+        sum += k.f32 ? clip_squares<true>(t.grad[k.tensor], k.at, k.length) : clip_squares<false>(t.grad[k.tensor], k.at, k.length);
+    }
+    sum = clip_sum<kClipThreads>(sum, part);
+    if (threadIdx.x == 0) parts[blockIdx.x] = sum;
+}
+
+// parts[count]: where the factor goes
+__global__ __launch_bounds__(1024) void clip_join_kernel(int64_t count, double *parts, double max_norm, float *norm)
+{
+    __shared__ double part[1024];
+    double sum = 0.0;
+    for (int64_t i = threadIdx.x; i < count; i += 1024) sum += parts[i];
+    sum = clip_sum<1024>(sum, part);
+    if (threadIdx.x == 0) {
+        const double all = sqrt(sum);
+        *norm = (float)all;
+        parts[count] = all > max_norm && all < INFINITY ? max_norm / all : 1.0;
+    }
+}
+
+template <bool F32>
+__device__ __forceinline__ void clip_scale(const void *grad, void *out, int64_t at, int length, double factor)
+{
+    const auto *v = static_cast<const typename Values<F32>::T *>(grad) + at;
+    auto *o = static_cast<typename Values<F32>::T *>(out) + at;
+#pragma unroll 4
+    for (int col = threadIdx.x * 8; col < length; col += kClipThreads * 8) {
+        float x[8];
+        Values<F32>::load(v, col, length, x);
+        // (in 64 bits: a factor below 2^-126 would lose bits as a float)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) x[q] = (float)((double)x[q] * factor);
+        Values<F32>::store(o, col, length, x);
+    }
+}
+
+__global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(ClipTable t, const double *at)
+{
+    const double factor = *at;
+    const int chunks = t.first[t.n];
+    for (int i = (int)blockIdx.x; i < chunks; i += (int)gridDim.x) {
+        // from the end: what was read last is still in the caches
+        const ClipChunk k = clip_chunk(t, chunks - 1 - i);
+        if (factor == 1.0 && t.out[k.tensor] == t.grad[k.tensor]) continue;
+        if (k.f32) clip_scale<true>(t.grad[k.tensor], t.out[k.tensor], k.at, k.length, factor);
+        else clip_scale<false>(t.grad[k.tensor], t.out[k.tensor], k.at, k.length, factor);
+    }
+}
+
+// Tensors [from, to) of a launch and its chunks; empty ones are left out.  A launch ends before its chunks pass 2^30.
+struct ClipRange { int to, tensors; int64_t chunks; };
+static ClipRange clip_range(int n, const int64_t *counts, int from)
+{
+    ClipRange r{from, 0, 0};
+    for (; r.to < n && r.tensors < kClipTensors; ++r.to) {
+        if (counts[r.to] <= 0) continue;
+        const int64_t chunks = (counts[r.to] + kChunk - 1) / kChunk;
+        if (r.tensors > 0 && r.chunks + chunks > 1 << 30) break;
+        r.chunks += chunks;
+        ++r.tensors;
+    }
+    return r;
+}
+static int clip_blocks(int64_t chunks) { return (int)(chunks < kClipBlocks ? chunks : kClipBlocks); }
+
+static int64_t clip_parts(int n, const int64_t *counts)
+{
+    int64_t parts = 0;
+    for (int from = 0; from < n;) {
+        const ClipRange r = clip_range(n, counts, from);
+        parts += clip_blocks(r.chunks);
+        from = r.to;
+    }
+    return parts;
+}
+
+size_t clip_workspace_bytes(int n, const int64_t *counts) { return (size_t)(clip_parts(n, counts) + 1) * sizeof(double); }
+
+hipError_t clip_launch(int n, const void *const *grads, const int64_t *counts, const int *types, double max_norm, void *const *out, float *norm,
+                       void *workspace, hipStream_t st)
+{
+    double *parts = static_cast<double *>(workspace);
+    const int64_t all = clip_parts(n, counts);
+    const auto each = [&](auto launch) {
+        int64_t before = 0;
+        for (int from = 0; from < n;) {
+            const ClipRange r = clip_range(n, counts, from);
+            ClipTable t{};
+            for (int i = from; i < r.to; ++i) {
+                if (counts[i] <= 0) continue;
+                t.grad[t.n] = grads[i];
+                t.out[t.n] = out ? out[i] : nullptr;
+                t.count[t.n] = counts[i];
+                t.first[t.n + 1] = t.first[t.n] + (int)((counts[i] + kChunk - 1) / kChunk);
+                if (types[i] == POLYDL_F32) t.f32[t.n >> 5] |= 1u << (t.n & 31);
+                ++t.n;
+            }
+            const hipError_t e = t.n ? launch(t, clip_blocks(r.chunks), parts + before) : hipSuccess;
+            if (e != hipSuccess) return e;
+            before += clip_blocks(r.chunks);
+            from = r.to;
+        }
+        return hipSuccess;
+    };
+    hipError_t e = each([&](const ClipTable &t, int blocks, double *at) {
+        return launch_kernel(clip_squares_kernel, dim3((unsigned)blocks), dim3(kClipThreads), 0, st, t, at);
+    });
+    if (e == hipSuccess) e = launch_kernel(clip_join_kernel, dim3(1), dim3(1024), 0, st, all, parts, max_norm, norm);
+    if (e != hipSuccess || !out) return e;
+    return each([&](const ClipTable &t, int blocks, double *) {
+        return launch_kernel(clip_scale_kernel, dim3((unsigned)blocks), dim3(kClipThreads), 0, st, t, (const double *)(parts + all));
+    });
+}
+
+}  // namespace polydl

@@ -1,0 +1,176 @@
+"""What a training step needs around a layer of experts: ctypes binding of the layer norm, the router's balance loss, the norm of all gradients
+and their clipping (same names as the C entry points, argument marshalling only).
+
+As in the layer of experts, gradients are calls of their own, results carry no graph, and nothing here waits for the device.  Matrices may have
+any row stride; their columns are contiguous.
+
+`stream` (None: torch's current stream) is where a call runs.  What it allocates is that stream's memory; as with any work on several streams, the
+caller makes `stream` wait for the arguments, keeps them until it has read them, and waits for it before using the results elsewhere."""
+import collections
+import ctypes
+
+import torch
+
+from .binding import _check, _new, _stream_ptr, lib
+from .experts import _dense, _device, _matrix, _no_graph, _type
+
+_i, _p, _l, _z, _f, _d = ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float, ctypes.c_double
+for _name, _args in {
+        "polydl_layernorm_fwd": [_i, _i, _p, _l, _i, _p, _p, _f, _p, _l, _i, _p, _p, _p],
+        "polydl_layernorm_bwd": [_i, _i, _p, _l, _i, _p, _l, _i, _p, _p, _p, _p, _l, _p, _p, _i, _p, _z, _p],
+        "polydl_balance": [_i] * 3 + [_p] * 7 + [_z, _p],
+        "polydl_balance_bwd": [_i, _i, _p, _p, _p, _f, _p, _p, _i, _p],
+        "polydl_grad_norm": [_i, _p, _p, _p, _p, _p, _z, _p],
+        "polydl_clip_grads": [_i, _p, _p, _p, _d, _p, _p, _p, _z, _p]}.items():
+    getattr(lib, _name).argtypes = _args
+    getattr(lib, _name).restype = _i
+for _name, _args in {"polydl_layernorm_bwd_workspace_bytes": [_i, _i], "polydl_balance_workspace_bytes": [_i, _i],
+                     "polydl_clip_workspace_bytes": [_i, _p]}.items():
+    getattr(lib, _name).argtypes = _args
+    getattr(lib, _name).restype = _z
+
+Norm = collections.namedtuple("Norm", "y mean rstd")
+NormGradients = collections.namedtuple("NormGradients", "dx dgamma dbeta")
+Balance = collections.namedtuple("Balance", "loss counts shares rows")
+
+
+def _lost(*tensors):
+    """Refuses arguments whose gradient would be lost."""
+    if torch.is_grad_enabled() and any(isinstance(t, torch.Tensor) and t.requires_grad for t in tensors):
+        _no_graph()
+
+
+def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, out=None, out_dtype=None, stream=None):
+    """polydl_layernorm_fwd on the rows of x [T][D] (float32 or bfloat16): Norm(y [T][D] of out_dtype (None: x's), mean [T], rstd [T])."""
+    _lost(x, gamma, beta)
+    (T, D), dev = x.shape, _device()
+    if out is None:
+        out = _new((T, D), x.dtype if out_dtype is None else out_dtype, x, stream)
+    mean, rstd = _new((2, T), torch.float32, x, stream).unbind(0)
+    xp, ldx = _matrix(x, "x", x.dtype, (T, D), dev)
+    yp, ldy = _matrix(out, "out", out.dtype, (T, D), dev)
+    _check(lib.polydl_layernorm_fwd(T, D, xp, ldx, _type(x.dtype), _dense(gamma, "gamma", torch.float32, (D,), dev),
+                                    _dense(beta, "beta", torch.float32, (D,), dev), eps, yp, ldy, _type(out.dtype), mean.data_ptr(), rstd.data_ptr(),
+                                    _stream_ptr(stream)), "polydl_layernorm_fwd")
+    return Norm(out, mean, rstd)
+
+
+def layernorm_bwd(dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, accumulate=False, weights=True, stream=None):
+    """polydl_layernorm_bwd: NormGradients(dx [T][D] of x's type, dgamma [D], dbeta [D] float32).  accumulate adds to the dgamma and dbeta that
+    are given; weights=False leaves them out (None)."""
+    (T, D), dev = x.shape, _device()
+    if not weights and (accumulate or dgamma is not None or dbeta is not None):
+        raise ValueError("weights=False forms neither dgamma nor dbeta")
+    if accumulate and (dgamma is None or dbeta is None):
+        raise ValueError("accumulate needs dgamma and dbeta")
+    if dx is None:
+        dx = _new((T, D), x.dtype, x, stream)
+    if weights and dgamma is None:
+        dgamma = _new((D,), torch.float32, x, stream)
+    if weights and dbeta is None:
+        dbeta = _new((D,), torch.float32, x, stream)
+    need = lib.polydl_layernorm_bwd_workspace_bytes(T, D) if weights else 0
+    space = _new((need,), torch.uint8, x, stream) if need else None
+    dp, lddy = _matrix(dy, "dy", dy.dtype, (T, D), dev)
+    xp, ldx = _matrix(x, "x", x.dtype, (T, D), dev)
+    op, lddx = _matrix(dx, "dx", x.dtype, (T, D), dev)
+    _check(lib.polydl_layernorm_bwd(T, D, dp, lddy, _type(dy.dtype), xp, ldx, _type(x.dtype), _dense(mean, "mean", torch.float32, (T,), dev),
+                                    _dense(rstd, "rstd", torch.float32, (T,), dev), _dense(gamma, "gamma", torch.float32, (D,), dev), op, lddx,
+                                    _dense(dgamma, "dgamma", torch.float32, (D,), dev), _dense(dbeta, "dbeta", torch.float32, (D,), dev),
+                                    bool(accumulate), space.data_ptr() if need else None, need, _stream_ptr(stream)), "polydl_layernorm_bwd")
+    return NormGradients(dx, dgamma, dbeta)
+
+
+def balance(logits, ids, stream=None):
+    """polydl_balance on a router's logits [T][E] and choices [T][k]: Balance(loss [], counts [E] int32, shares [E], rows [] int32)."""
+    _lost(logits)
+    (T, E), k, dev = logits.shape, ids.shape[1], _device()
+    src = _dense(logits, "logits", torch.float32, (T, E), dev)
+    loss, shares, counts, rows = _new((2 * E + 2,), torch.int32, logits, stream).split_with_sizes((1, E, E, 1))     # one allocation
+    need = lib.polydl_balance_workspace_bytes(T, E)
+    space = _new((need,), torch.uint8, logits, stream) if need else None
+    _check(lib.polydl_balance(T, E, k, src, _dense(ids, "ids", torch.int32, (T, k), dev), loss.data_ptr(), counts.data_ptr(), shares.data_ptr(),
+                              rows.data_ptr(), space.data_ptr() if need else None, need, _stream_ptr(stream)), "polydl_balance")
+    return Balance(loss.view(torch.float32)[0], counts, shares.view(torch.float32), rows[0])
+
+
+def balance_bwd(logits, counts, rows, dloss=1.0, out=None, accumulate=False, stream=None):
+    """polydl_balance_bwd: the gradient of the logits [T][E] from that of the loss, a number or a float32 tensor of one value; accumulate adds it
+    to out."""
+    (T, E), dev = logits.shape, _device()
+    if accumulate and out is None:
+        raise ValueError("accumulate needs out")
+    if out is None:
+        out = _new((T, E), torch.float32, logits, stream)
+    given = isinstance(dloss, torch.Tensor)
+    for t, name in ((rows, "rows"),) + (((dloss, "dloss"),) if given else ()):
+        if t.numel() != 1:
+            raise ValueError("%s must hold one value" % name)
+    _check(lib.polydl_balance_bwd(T, E, _dense(logits, "logits", torch.float32, (T, E), dev), _dense(counts, "counts", torch.int32, (E,), dev),
+                                  _dense(rows, "rows", torch.int32, rows.shape, dev), 1.0 if given else dloss,
+                                  _dense(dloss, "dloss", torch.float32, dloss.shape, dev) if given else None,
+                                  _dense(out, "out", torch.float32, (T, E), dev), bool(accumulate), _stream_ptr(stream)), "polydl_balance_bwd")
+    return out
+
+
+def _filled(t):
+    """Whether a tensor's values lie without gaps or overlaps, in whatever order of its axes."""
+    if t.is_contiguous():
+        return True
+    step = 1
+    for stride, size in sorted((st, n) for st, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != step:
+            return False
+        step *= size
+    return True
+
+
+def _table(tensors, name, dev):
+    """Addresses, lengths and types of dense tensors as host arrays."""
+    for t in tensors:
+        if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, torch.bfloat16):
+            raise TypeError("%s must be float32 or bfloat16 tensors" % name)
+        if not t.is_cuda or t.get_device() != dev:
+            raise TypeError("%s must be in the current device's memory" % name)
+        if not _filled(t):
+            raise TypeError("%s must be dense" % name)
+    n = len(tensors)
+    return ((_p * n)(*[t.data_ptr() for t in tensors]), (_l * n)(*[t.numel() for t in tensors]),
+            (_i * n)(*[0 if t.dtype is torch.float32 else 1 for t in tensors]))
+
+
+def _norm_space(tensors, counts, stream):
+    if not tensors:
+        raise ValueError("there are no gradients")
+    need = lib.polydl_clip_workspace_bytes(len(tensors), counts)
+    return _new((1,), torch.float32, tensors[0], stream), _new((need,), torch.uint8, tensors[0], stream), need
+
+
+def grad_norm(grads, stream=None):
+    """polydl_grad_norm: the norm [] (float32) of a list of tensors (float32 or bfloat16, dense) taken as one vector."""
+    grads = list(grads)
+    _lost(*grads)
+    at, counts, types = _table(grads, "grads", _device())
+    norm, space, need = _norm_space(grads, counts, stream)
+    _check(lib.polydl_grad_norm(len(grads), at, counts, types, norm.data_ptr(), space.data_ptr(), need, _stream_ptr(stream)), "polydl_grad_norm")
+    return norm[0]
+
+
+def clip_grads(grads, max_norm, out=None, stream=None):
+    """polydl_clip_grads: scales a list of tensors to a norm of at most max_norm, in place or into the tensors of `out` (of the same types, shapes
+    and strides); returns the norm [] (float32) before.  Where that is not finite, nothing is scaled."""
+    grads = list(grads)
+    _lost(*grads)
+    dev = _device()
+    at, counts, types = _table(grads, "grads", dev)
+    to = None
+    if out is not None:
+        out = list(out)
+        if len(out) != len(grads) or any(o.dtype != t.dtype or o.shape != t.shape or (not t.is_contiguous() or not o.is_contiguous()) and
+                                         o.stride() != t.stride() for o, t in zip(out, grads)):
+            raise ValueError("out must be tensors of the gradients' types, shapes and strides")
+        to = _table(out, "out", dev)[0]
+    norm, space, need = _norm_space(grads, counts, stream)
+    _check(lib.polydl_clip_grads(len(grads), at, counts, types, float(max_norm), to, norm.data_ptr(), space.data_ptr(), need, _stream_ptr(stream)),
+           "polydl_clip_grads")
+    return norm[0]
