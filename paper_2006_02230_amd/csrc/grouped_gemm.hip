@@ -16,26 +16,23 @@
 // last, the reduction's tail.  The kernel reads the group of its tile from the offsets in device memory, so nothing waits for
 // the host.
 #include <hip/hip_runtime.h>
-#include <atomic>
 #include <type_traits>
 #include "blocks.hpp"
 #include "experts.hpp"
 #include "gemm_core.hpp"
 #include "group_tiles.hpp"
 #include "internal.hpp"
+#include "lds_loads.hpp"
 
 namespace polydl {
 
 typedef __bf16 gg_bf16x8 __attribute__((ext_vector_type(8)));
 typedef float gg_f32x4 __attribute__((ext_vector_type(4)));
 typedef short gg_i16x4 __attribute__((ext_vector_type(4)));
-typedef int gg_i32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t gg_u32x2 __attribute__((ext_vector_type(2)));
 
 constexpr int kStage = 64;                          // reduction of a stage: two matrix instructions' of 32
 constexpr int kIndices = 4096;                      // row indices of the reduction kept in LDS at a time
-constexpr uint32_t kFarOffset = 0xfffffff0u;        // out of range of every descriptor here
-constexpr uint64_t kFarRecords = 0xffffffe0ull;     // so that no sum of an offset in range and a load's width reaches 2^32
 
 struct GroupedArgs {
     int E, M, out_rows, cols, red;
@@ -51,36 +48,6 @@ struct GroupedArgs {
     int row_tiles, col_tiles;      // of one C_e (GROUPED_DW); columns (others)
 };
 
-// A raw buffer descriptor of `bytes` bytes from base (none if negative), in operations of 32 bits: there are no scalar comparisons of 64.
-__device__ __forceinline__ gg_i32x4 gg_rsrc(uint64_t base, int64_t bytes)
-{
-    const int high = (int)(bytes >> 32);
-    const uint32_t low = (uint32_t)bytes, most = (uint32_t)kFarRecords;
-    const uint32_t n = high < 0 ? 0u : high > 0 ? most : low < most ? low : most;
-    return gg_i32x4{(int)(uint32_t)base, (int)((uint32_t)(base >> 32) & 0xffffu), (int)n, 0x00020000};
-}
-// Sixteen bytes a lane into LDS at `lds` + 16 * lane; not waited for.  As assembly, because the compiler puts a wait for every such
-// load before each transposing LDS read, whichever buffer it reads (measured with stages of 32 at 16384 x 4096 x 2048: dX 1112
-// against 902, dW 865 against 512 TFLOP/s).  No register is written; the waits are gg_wait()'s.  m0, where the
-// load's LDS address is, is an operand that the compiler sets and knows of; the wait states are those that a descriptor or m0 just written needs.
-__device__ __forceinline__ void gg_dma(gg_i32x4 rsrc, uint32_t lds, uint32_t off)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    asm volatile("s_nop 4\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds" ::"{m0}"(lds), "v"(off), "s"(rsrc) : "memory");
-#else
-    (void)rsrc; (void)lds; (void)off;
-#endif
-}
-// where a pointer into the workgroup's LDS points
-__device__ __forceinline__ uint32_t gg_lds_offset(const char *lds)
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    return (uint32_t)(uintptr_t)(const __attribute__((address_space(3))) char *)lds;
-#else
-    (void)lds;
-    return 0;
-#endif
-}
 __device__ __forceinline__ gg_u32x2 gg_read_tr(const char *lds)
 {
 #if defined(__HIP_DEVICE_COMPILE__)
@@ -243,15 +210,6 @@ struct Operand {
         }
     }
 };
-
-// s_waitcnt of the gfx9 encoding: vmcnt N (bits 3:0, 15:14), lgkmcnt 0 (11:8), expcnt left alone
-template <int N>
-__device__ __forceinline__ void gg_wait()
-{
-#if defined(__HIP_DEVICE_COMPILE__)
-    __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4 << 14) | 0x70);
-#endif
-}
 
 // four floats at any of their addresses
 typedef gg_f32x4 __attribute__((aligned(4))) Floats4;
@@ -639,21 +597,6 @@ __global__ __launch_bounds__(T::kThreads) void grouped_kernel(GroupedArgs p)
             now = next;
         }
     }
-}
-
-// More LDS than the default window has to be asked for, once per kernel and device.
-template <auto KERNEL>
-static hipError_t ask_lds(int bytes)
-{
-    static std::atomic<uint64_t> asked{0};
-    int dev = 0;
-    hipError_t e = hipGetDevice(&dev);
-    if (e != hipSuccess) return e;
-    const uint64_t bit = dev < 64 ? 1ull << dev : 0;
-    if (asked.load(std::memory_order_relaxed) & bit) return hipSuccess;
-    e = hipFuncSetAttribute(reinterpret_cast<const void *>(KERNEL), hipFuncAttributeMaxDynamicSharedMemorySize, bytes);
-    if (e == hipSuccess) asked.fetch_or(bit, std::memory_order_relaxed);
-    return e;
 }
 
 template <int FORM, int BM, int BN, int WM, int WN, int BUFFERS, bool DMA, bool GATHER, bool OUT_F32, bool PAST>

@@ -176,6 +176,33 @@ def test_product(P, E, M, N, K, gather, out):
     check(got, want, m, K, out)
 
 
+# what the rule gives tiles of 64, 128 and 256, each with whole tiles, edges, groups of no rows, one to five stages and rows of less than 16 scales; several tiles a
+# workgroup
+TILES = [(1, 70, 130, k) for k in (30, 100, 256, 300, 400, 513, 1000, 1300)] + [(4, 9000, 1000, 130), (3, 12000, 700, 500)] + \
+    [(1, 2100, 2300, k) for k in (100, 400, 600)] + [(5, 1900, 2100, 300)] + [(1, 4096, 4100, k) for k in (96, 384, 777)] + [(6, 9001, 3001, 257), (3, 20000, 2050, 128)]
+
+
+@pytest.mark.parametrize("E,M,N,K", TILES)
+def test_tiles(P, E, M, N, K):
+    import torch
+    g = gen(M + K)
+    # the reference on the GPU in 64 bits: the values are exact there, and so is their product up to its own sums' 2^-53
+    x, w = P.mx4_quantise(randn(g, M, K).bfloat16()), P.mx4_quantise(randn(g, E, N, K) * K ** -0.5)
+    offsets = offsets_of(g, E, M, 3)
+    xv, wv = P.mx4_dequantise(x, K, out_dtype=torch.float32).double(), P.mx4_dequantise(w, K, out_dtype=torch.float32).double()
+    rows = torch.randint(0, M, (M,), generator=g, device="cuda").int() if K % 2 else None
+    if rows is not None:
+        xv = xv[rows.long()]
+    name, act = ("bf16", "relu") if K % 3 else ("f32", None)
+    got = P.mx4_gemm(x, w, offsets=offsets, rows=rows, act=act, out_dtype=kind(name))
+    o = offsets.tolist()
+    for e in range(E):
+        a, b = o[e], o[e + 1]
+        y, m = xv[a:b] @ wv[e].T, xv[a:b].abs() @ wv[e].abs().T
+        check(got[a:b], (y.clamp(min=0) if act else y).cpu().numpy(), m.cpu().numpy(), K, name)
+    assert not got[o[E]:].any()
+
+
 @pytest.mark.parametrize("E,M,N,K", [(1, 2, 40, 200), (3, 90, 100, 130), (2, 600, 300, 256)])
 def test_product_into_rows_of_a_longer_tensor(P, E, M, N, K):
     import torch
@@ -233,6 +260,21 @@ def test_broken_blocks_reach_their_row_or_column_alone(P, M):
     assert bool(torch.isnan(got[broken]).all()) and torch.equal(got[~broken], good[~broken])
     for act in ("relu", "relu6"):
         assert bool(torch.isnan(P.mx4_gemm(P.mx4_quantise(a), P.mx4_quantise(b), act=act)[broken]).all())
+
+
+def test_rows_by_index_past_4_gib(P):
+    # rows on both sides of 2^32 bytes, which no 32-bit offset reaches; the others are never read
+    import torch
+    g = gen(77)
+    K, M, N = 8192, 40, 70
+    x_rows = (1 << 20) + 50
+    q, s = torch.empty((x_rows, K // 2), dtype=torch.uint8, device="cuda"), torch.empty((x_rows, K // 32), dtype=torch.uint8, device="cuda")
+    rows = torch.cat([torch.arange(20, device="cuda"), torch.arange(x_rows - 20, x_rows, device="cuda")])
+    x, w = P.mx4_quantise(randn(g, M, K)), P.mx4_quantise(randn(g, N, K))
+    q[rows], s[rows] = x.q, x.scales
+    got = P.mx4_gemm(P.Mx4(q, s), w, rows=rows.int(), out_dtype=torch.float32)
+    want, m = product(values(P, x, K), values(P, w, K)[None], None, None, None, N)
+    check(got, want, m, K, "f32")
 
 
 def test_results_do_not_depend_on_the_run_or_the_other_rows(P):
