@@ -25,15 +25,23 @@ __device__ __forceinline__ float balance_value(uint32_t key)
     return __builtin_bit_cast(float, key >> 31 ? key ^ 0x80000000u : ~key);
 }
 
-// p: the lane's NV probabilities of a row (NULL: none, zeros).  False where no expert is open.
+// The lane's NV logits of a row (NULL: none, all masked)
 template <int LANES, int NV>
-__device__ __forceinline__ bool balance_row(const float *row, int E, int l, float (&p)[NV])
+__device__ __forceinline__ void balance_load(const float *row, int E, int l, float (&v)[NV])
+{
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int e = i * LANES + l;
+        v[i] = row && e < E ? row[e] : -INFINITY;
+    }
+}
+// Logits to probabilities, zeros where no expert is open: then false.
+template <int LANES, int NV>
+__device__ __forceinline__ bool balance_row(float (&p)[NV])
 {
     uint32_t m = 0u;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
-        const int e = i * LANES + l;
-        p[i] = row && e < E ? row[e] : -INFINITY;
         const uint32_t key = balance_key(p[i]);
         m = key > m ? key : m;
     }
@@ -51,14 +59,11 @@ __device__ __forceinline__ bool balance_row(const float *row, int E, int l, floa
     return m != 0u;
 }
 
-constexpr int kBalanceThreads = 512, kBalanceWaves = kBalanceThreads / 64;
-
 struct BalanceArgs {
     BalanceProblem p;
     int blocks, per;                // workgroups, rows of one
     float *part;                    // [blocks][E]: sums of probabilities
-    int32_t *count;                 // [blocks][E]
-    int32_t *open;                  // [blocks]
+    int32_t *count;                 // [blocks][E+1]: choices, open rows
 };
 
 // loss and shares from the sums of probabilities and the counts, in LDS; the whole workgroup
@@ -73,49 +78,62 @@ __device__ __forceinline__ void balance_finish(const BalanceProblem &p, const fl
         total += (double)counts[e];
         product += (double)counts[e] * (double)share;
     }
-    part[threadIdx.x] = total;
-    part[THREADS + threadIdx.x] = product;
-    for (int n = THREADS / 2; n > 0; n >>= 1) {
-        __syncthreads();
-        if ((int)threadIdx.x < n) {
-            part[threadIdx.x] += part[threadIdx.x + n];
-            part[THREADS + threadIdx.x] += part[THREADS + threadIdx.x + n];
-        }
+    // in a wave, then the waves in their order
+#pragma unroll
+    for (int x = 1; x < 64; x += x) {
+        total += __shfl_xor(total, x);
+        product += __shfl_xor(product, x);
     }
-    if (threadIdx.x == 0) {
-        // NaN shares make the loss NaN without choices too
-        *p.loss = (float)((double)p.E * (part[0] > 0.0 ? part[THREADS] / part[0] : part[THREADS]));
-        *p.rows = rows;
+    if ((threadIdx.x & 63) == 0) {
+        part[threadIdx.x >> 6] = total;
+        part[THREADS / 64 + (threadIdx.x >> 6)] = product;
     }
+    __syncthreads();
+    if (threadIdx.x != 0) return;
+    for (int w = 1; w < THREADS / 64; ++w) {
+        total += part[w];
+        product += part[THREADS / 64 + w];
+    }
+    // (NaN shares make the loss NaN without choices too)
+    *p.loss = (float)((double)p.E * (total > 0.0 ? product / total : product));
+    *p.rows = rows;
 }
 
-template <int LANES, int NV, bool ONE>
-__global__ __launch_bounds__(kBalanceThreads) void balance_kernel(BalanceArgs a)
+// ONE: the workgroup is the only one, and the loss is formed here too.
+template <int LANES, int NV, int THREADS, bool ONE>
+__global__ __launch_bounds__(THREADS) void balance_kernel(BalanceArgs a)
 {
-    constexpr int kExperts = LANES * NV;
-    __shared__ float sums[kBalanceWaves][kExperts];
-    __shared__ int counts[kExperts], open[kBalanceWaves];
-    __shared__ double part[ONE ? 2 * kBalanceThreads : 1];
+    constexpr int kExperts = LANES * NV, kWaves = THREADS / 64, kRows = THREADS / LANES;
+    __shared__ float sums[kWaves][kExperts];
+    __shared__ int counts[kExperts], open[kWaves];
+    __shared__ double part[ONE ? 2 * kWaves : 1];
     const BalanceProblem &p = a.p;
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l = tid % LANES, b = (int)blockIdx.x;
-    const int64_t t0 = (int64_t)b * a.per, t1 = min((int64_t)p.T, t0 + a.per);
-    for (int e = tid; e < kExperts; e += kBalanceThreads) counts[e] = 0;
-    __syncthreads();
-    for (int64_t i = t0 * p.k + tid; i < t1 * p.k; i += kBalanceThreads) {
-        const int id = p.ids[i];
-        if ((unsigned)id < (unsigned)p.E) atomicAdd(&counts[id], 1);
-    }
-    float acc[NV];
+    const int64_t t0 = (int64_t)b * a.per, t1 = min((int64_t)p.T, t0 + a.per), i0 = t0 * p.k + tid, i1 = t1 * p.k;
+    // the next rows are on their way while these are worked on, the first choices meanwhile, too
+    const auto load = [&](int64_t t, float (&v)[NV]) {
+        const int64_t at = t + tid / LANES;
+        balance_load<LANES, NV>(at < t1 ? p.logits + at * p.E : nullptr, p.E, l, v);
+    };
+    float acc[NV], v[NV], next[NV];
+    load(t0, v);
+    const int first = i0 < i1 ? p.ids[i0] : -1;
+    for (int e = tid; e < kExperts; e += THREADS) counts[e] = 0;
     int rows = 0;
 #pragma unroll
     for (int i = 0; i < NV; ++i) acc[i] = 0.f;
-    for (int64_t t = t0; t < t1; t += kBalanceThreads / LANES) {
-        const int64_t at = t + tid / LANES;
-        float v[NV];
-        const bool is = balance_row<LANES, NV>(at < t1 ? p.logits + at * p.E : nullptr, p.E, l, v);
+    for (int64_t t = t0; t < t1; t += kRows) {
+        load(t + kRows, next);
+        const bool is = balance_row<LANES, NV>(v);
         rows += is && l == 0;
 #pragma unroll
-        for (int i = 0; i < NV; ++i) acc[i] += v[i];
+        for (int i = 0; i < NV; ++i) { acc[i] += v[i]; v[i] = next[i]; }
+    }
+    __syncthreads();                    // counts
+    if ((unsigned)first < (unsigned)p.E) atomicAdd(&counts[first], 1);
+    for (int64_t i = i0 + THREADS; i < i1; i += THREADS) {
+        const int id = p.ids[i];
+        if ((unsigned)id < (unsigned)p.E) atomicAdd(&counts[id], 1);
     }
     // the rows of a wave, then the waves
 #pragma unroll
@@ -129,52 +147,77 @@ __global__ __launch_bounds__(kBalanceThreads) void balance_kernel(BalanceArgs a)
     if (lane == 0) open[wave] = rows;
     __syncthreads();
     rows = 0;
-    for (int w = 0; w < kBalanceWaves; ++w) rows += open[w];
-    for (int e = tid; e < p.E; e += kBalanceThreads) {
+    for (int w = 0; w < kWaves; ++w) rows += open[w];
+    for (int e = tid; e < p.E; e += THREADS) {
         float sum = sums[0][e];
-        for (int w = 1; w < kBalanceWaves; ++w) sum += sums[w][e];
+        for (int w = 1; w < kWaves; ++w) sum += sums[w][e];
         if constexpr (ONE) {
             sums[0][e] = sum;
         } else {
             a.part[(int64_t)b * p.E + e] = sum;
-            a.count[(int64_t)b * p.E + e] = counts[e];
+            a.count[(int64_t)b * (p.E + 1) + e] = counts[e];
         }
     }
     if constexpr (ONE) {
         __syncthreads();
-        balance_finish<kBalanceThreads>(p, sums[0], counts, rows, part);
+        balance_finish<THREADS>(p, sums[0], counts, rows, part);
     } else if (tid == 0) {
-        a.open[b] = rows;
+        a.count[(int64_t)b * (p.E + 1) + p.E] = rows;
     }
 }
 
-// The workgroups' sums.
+// The workgroups' sums.  A thread takes an expert of every SLICES-th workgroup; the slices meet in LDS in their order.
+template <int SLICES>
 __global__ __launch_bounds__(1024) void balance_join_kernel(BalanceArgs a)
 {
-    __shared__ float sums[kRouteMaxExperts];
-    __shared__ int counts[kRouteMaxExperts];
-    __shared__ double part[2 * 1024];
-    int rows = 0;
-    for (int b = 0; b < a.blocks; ++b) rows += a.open[b];
-    for (int e = threadIdx.x; e < a.p.E; e += 1024) {
-        float sum = 0.f;
-        int count = 0;
-        for (int b = 0; b < a.blocks; ++b) {
-            sum += a.part[(int64_t)b * a.p.E + e];
-            count += a.count[(int64_t)b * a.p.E + e];
+    constexpr int kAcross = 1024 / SLICES;
+    __shared__ float sums[SLICES][kAcross + 1];
+    __shared__ int counts[SLICES][kAcross + 1];
+    __shared__ double part[2 * 16];
+    const int e = threadIdx.x % kAcross, slice = threadIdx.x / kAcross, E = a.p.E;
+    float sum = 0.f;
+    int count = 0, rows = 0;
+    for (int b = (int)(threadIdx.x & 63); b < a.blocks; b += 64) rows += a.count[(int64_t)b * (E + 1) + E];
+    // sixteen workgroups' at a time are on their way: they come from other dies, 2 us each time (four at a time: 16384 x 128 19.6 us)
+    constexpr int kHeld = 16;
+    for (int b0 = slice; b0 < a.blocks; b0 += SLICES * kHeld) {
+        float s[kHeld];
+        int c[kHeld];
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int b = b0 + i * SLICES;
+            const bool there = e < E && b < a.blocks;
+            s[i] = there ? a.part[(int64_t)b * E + e] : 0.f;
+            c[i] = there ? a.count[(int64_t)b * (E + 1) + e] : 0;
         }
-        sums[e] = sum;
-        counts[e] = count;
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            sum += s[i];
+            count += c[i];
+        }
+    }
+    rows = lane_of(wave_prefix(rows), 63);
+    sums[slice][e] = sum;
+    counts[slice][e] = count;
+    __syncthreads();
+    if (slice == 0) {
+        for (int s = 1; s < SLICES; ++s) {
+            sum += sums[s][e];
+            count += counts[s][e];
+        }
+        sums[0][e] = sum;
+        counts[0][e] = count;
     }
     __syncthreads();
-    balance_finish<1024>(a.p, sums, counts, rows, part);
+    balance_finish<1024>(a.p, sums[0], counts[0], rows, part);
 }
 
-// Rows of a workgroup at least, and workgroups at most.
+// Rows of a workgroup at least, and workgroups at most: a row a group of lanes, four times; one workgroup adds the others' sums up.
+constexpr int kBalanceRows = 256, kBalanceBlocks = 128;
 static int balance_blocks(int T)
 {
-    const int64_t blocks = ((int64_t)T + 127) / 128;
-    return blocks < 1 ? 1 : blocks < 64 ? (int)blocks : 64;
+    const int64_t blocks = T <= kBalanceRows ? 1 : ((int64_t)T + 63) / 64;
+    return (int)(blocks < kBalanceBlocks ? blocks : kBalanceBlocks);
 }
 
 size_t balance_workspace_bytes(int T, int E)
@@ -186,18 +229,18 @@ size_t balance_workspace_bytes(int T, int E)
 template <int LANES, int NV>
 static hipError_t balance_run(const BalanceArgs &a, hipStream_t st)
 {
-    if (a.blocks <= 1) return launch_kernel((balance_kernel<LANES, NV, true>), dim3(1), dim3(kBalanceThreads), 0, st, a);
-    return launch_kernel((balance_kernel<LANES, NV, false>), dim3((unsigned)a.blocks), dim3(kBalanceThreads), 0, st, a);
+    constexpr int threads = LANES == 64 ? 512 : 1024;        // (more waves' sums of up to 1024 experts would not fit in LDS)
+    if (a.blocks <= 1) return launch_kernel((balance_kernel<LANES, NV, threads, true>), dim3(1), dim3(threads), 0, st, a);
+    return launch_kernel((balance_kernel<LANES, NV, threads, false>), dim3((unsigned)a.blocks), dim3(threads), 0, st, a);
 }
 
 hipError_t balance_launch(const BalanceProblem &p, void *workspace, hipStream_t st)
 {
-    BalanceArgs a{p, balance_blocks(p.T), 0, nullptr, nullptr, nullptr};
+    BalanceArgs a{p, balance_blocks(p.T), 0, nullptr, nullptr};
     a.per = (int)(((int64_t)p.T + a.blocks - 1) / a.blocks);
     if (a.blocks > 1) {
         a.part = static_cast<float *>(workspace);
         a.count = reinterpret_cast<int32_t *>(a.part + (size_t)a.blocks * p.E);
-        a.open = a.count + (size_t)a.blocks * p.E;
     }
     auto *f = p.E <= 16    ? balance_run<16, 1>
               : p.E <= 32  ? balance_run<16, 2>
@@ -208,7 +251,13 @@ hipError_t balance_launch(const BalanceProblem &p, void *workspace, hipStream_t 
                            : balance_run<64, 16>;
     const hipError_t e = f(a, st);
     if (e != hipSuccess || a.blocks <= 1) return e;
-    return launch_kernel(balance_join_kernel, dim3(1), dim3(1024), 0, st, a);
+    auto *join = p.E <= 32    ? balance_join_kernel<32>
+                 : p.E <= 64  ? balance_join_kernel<16>
+                 : p.E <= 128 ? balance_join_kernel<8>
+                 : p.E <= 256 ? balance_join_kernel<4>
+                 : p.E <= 512 ? balance_join_kernel<2>
+                              : balance_join_kernel<1>;
+    return launch_kernel(join, dim3(1), dim3(1024), 0, st, a);
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
@@ -229,7 +278,8 @@ __global__ __launch_bounds__(256) void balance_bwd_kernel(int T, int E, const fl
     total = group_sum<LANES>(total);
     const int n = *rows;
     const float scale = coefficient * (dloss ? *dloss : 1.f) * (float)E / (float)max(n, 1);
-    balance_row<LANES, NV>(here ? logits + t * E : nullptr, E, l, p);
+    balance_load<LANES, NV>(here ? logits + t * E : nullptr, E, l, p);
+    balance_row<LANES, NV>(p);
     float mean = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {

@@ -12,7 +12,7 @@ import ctypes
 import torch
 
 from .binding import _check, _new, _stream_ptr, lib
-from .experts import _dense, _device, _matrix, _no_graph, _type
+from .experts import _TYPES, _dense, _device, _matrix, _no_graph, _type
 
 _i, _p, _l, _z, _f, _d = ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float, ctypes.c_double
 for _name, _args in {
@@ -125,52 +125,68 @@ def _filled(t):
     return True
 
 
-def _table(tensors, name, dev):
-    """Addresses, lengths and types of dense tensors as host arrays."""
-    for t in tensors:
-        if not isinstance(t, torch.Tensor) or t.dtype not in (torch.float32, torch.bfloat16):
-            raise TypeError("%s must be float32 or bfloat16 tensors" % name)
-        if not t.is_cuda or t.get_device() != dev:
-            raise TypeError("%s must be in the current device's memory" % name)
-        if not _filled(t):
+_Tensor = torch.Tensor
+
+
+# A check is one pass over the list: tensor by tensor, with calls for each, 300 tensors took 145 us.
+def _listed(tensors, name, dev):
+    """The types, lengths and layouts (None: all contiguous) of a list of dense tensors, checked."""
+    if not all([isinstance(t, _Tensor) for t in tensors]):
+        raise TypeError("%s must be tensors" % name)
+    types = [t.dtype for t in tensors]
+    if not set(types) <= {torch.float32, torch.bfloat16}:
+        raise TypeError("%s must be float32 or bfloat16 tensors" % name)
+    if set(map(_Tensor.get_device, tensors)) - {dev} or dev is None:
+        raise TypeError("%s must be in the current device's memory" % name)
+    layouts = None
+    if not all(map(_Tensor.is_contiguous, tensors)):
+        if not all(map(_filled, tensors)):
             raise TypeError("%s must be dense" % name)
-    n = len(tensors)
-    return ((_p * n)(*[t.data_ptr() for t in tensors]), (_l * n)(*[t.numel() for t in tensors]),
-            (_i * n)(*[0 if t.dtype is torch.float32 else 1 for t in tensors]))
+        layouts = [None if t.is_contiguous() else (t.shape, t.stride()) for t in tensors]
+    return types, list(map(_Tensor.numel, tensors)), layouts
 
 
-def _norm_space(tensors, counts, stream):
-    if not tensors:
+def _addresses(tensors):
+    return (_p * len(tensors))(*map(_Tensor.data_ptr, tensors))
+
+
+def _gradients(grads):
+    """The list, its types, lengths and layouts, and the host arrays of addresses, lengths and types that a call takes."""
+    grads = list(grads)
+    if not grads:
         raise ValueError("there are no gradients")
-    need = lib.polydl_clip_workspace_bytes(len(tensors), counts)
-    return _new((1,), torch.float32, tensors[0], stream), _new((need,), torch.uint8, tensors[0], stream), need
+    types, counts, layouts = _listed(grads, "grads", _device())
+    if torch.is_grad_enabled() and any([t.requires_grad for t in grads]):
+        _no_graph()
+    n = len(grads)
+    return grads, types, counts, layouts, _addresses(grads), (_l * n)(*counts), (_i * n)(*[_TYPES[t] for t in types])
+
+
+def _norm_space(like, n, counts, stream):
+    need = lib.polydl_clip_workspace_bytes(n, counts)
+    return _new((), torch.float32, like, stream), _new((need,), torch.uint8, like, stream), need
 
 
 def grad_norm(grads, stream=None):
     """polydl_grad_norm: the norm [] (float32) of a list of tensors (float32 or bfloat16, dense) taken as one vector."""
-    grads = list(grads)
-    _lost(*grads)
-    at, counts, types = _table(grads, "grads", _device())
-    norm, space, need = _norm_space(grads, counts, stream)
+    grads, _, _, _, at, counts, types = _gradients(grads)
+    norm, space, need = _norm_space(grads[0], len(grads), counts, stream)
     _check(lib.polydl_grad_norm(len(grads), at, counts, types, norm.data_ptr(), space.data_ptr(), need, _stream_ptr(stream)), "polydl_grad_norm")
-    return norm[0]
+    return norm
 
 
 def clip_grads(grads, max_norm, out=None, stream=None):
-    """polydl_clip_grads: scales a list of tensors to a norm of at most max_norm, in place or into the tensors of `out` (of the same types, shapes
-    and strides); returns the norm [] (float32) before.  Where that is not finite, nothing is scaled."""
-    grads = list(grads)
-    _lost(*grads)
-    dev = _device()
-    at, counts, types = _table(grads, "grads", dev)
+    """polydl_clip_grads: scales a list of tensors to a norm of at most max_norm, in place or into the tensors of `out` (of the same types and
+    lengths, and where they are not contiguous of the same shapes and strides); returns the norm [] (float32) before.  Where that is not finite,
+    nothing is scaled."""
+    grads, kinds, lengths, layouts, at, counts, types = _gradients(grads)
     to = None
     if out is not None:
         out = list(out)
-        if len(out) != len(grads) or any(o.dtype != t.dtype or o.shape != t.shape or (not t.is_contiguous() or not o.is_contiguous()) and
-                                         o.stride() != t.stride() for o, t in zip(out, grads)):
-            raise ValueError("out must be tensors of the gradients' types, shapes and strides")
-        to = _table(out, "out", dev)[0]
-    norm, space, need = _norm_space(grads, counts, stream)
+        if _listed(out, "out", _device()) != (kinds, lengths, layouts):
+            raise ValueError("out must be tensors of the gradients' types, lengths and layouts")
+        to = _addresses(out)
+    norm, space, need = _norm_space(grads[0], len(grads), counts, stream)
     _check(lib.polydl_clip_grads(len(grads), at, counts, types, float(max_norm), to, norm.data_ptr(), space.data_ptr(), need, _stream_ptr(stream)),
            "polydl_clip_grads")
-    return norm[0]
+    return norm
