@@ -6,6 +6,7 @@
 // Bound: HBM, every value read twice and written once; the 64-bit sums cost two instructions a value.
 #include <hip/hip_runtime.h>
 #include <math.h>
+#include <type_traits>
 #include "block.hpp"
 #include "blocks.hpp"
 #include "internal.hpp"
@@ -42,19 +43,48 @@ __device__ __forceinline__ ClipChunk clip_chunk(const ClipTable &t, int chunk)
     return {lo, (t.f32[lo >> 5] >> (lo & 31) & 1u) != 0u, at, (int)(left < kChunk ? left : kChunk)};
 }
 
-template <bool F32>
-__device__ __forceinline__ double clip_squares(const void *grad, int64_t at, int length)
+// A chunk's values, 16 bytes a load, the lanes of a wave side by side (eight floats a lane, in two loads 32 bytes apart: 134 M floats, squares 126 us).
+// use(values, n of them, where they begin in the chunk)
+template <bool F32, class USE>
+__device__ __forceinline__ void clip_each(const void *grad, const ClipChunk &k, USE use)
 {
-    const auto *v = static_cast<const typename Values<F32>::T *>(grad) + at;
-    double sum = 0.0;
-#pragma unroll 4
-    for (int col = threadIdx.x * 8; col < length; col += kClipThreads * 8) {
-        float x[8];
-        Values<F32>::load(v, col, length, x);
+    constexpr int kWide = F32 ? 4 : 8, kUnits = kChunk / (kClipThreads * kWide);
+    const auto *v = static_cast<const typename Values<F32>::T *>(grad) + k.at;
+    if (k.length == kChunk) {
+        lanes_u32x4 raw[kUnits];
 #pragma unroll
-        for (int q = 0; q < 8; ++q) sum += (double)x[q] * (double)x[q];
+        for (int i = 0; i < kUnits; ++i) raw[i] = reinterpret_cast<const Unit8 *>(v + (i * kClipThreads + (int)threadIdx.x) * kWide)->v;
+#pragma unroll
+        for (int i = 0; i < kUnits; ++i) {
+            float x[8];
+            if constexpr (F32) {
+                const values_f32x4 f = __builtin_bit_cast(values_f32x4, raw[i]);
+#pragma unroll
+                for (int q = 0; q < 4; ++q) x[q] = f[q];
+            } else {
+#pragma unroll
+                for (int q = 0; q < 4; ++q) { x[2 * q] = bf16_lo(raw[i][q]); x[2 * q + 1] = bf16_hi(raw[i][q]); }
+            }
+            use(x, std::integral_constant<int, kWide>{}, (i * kClipThreads + (int)threadIdx.x) * kWide);
+        }
+        return;
     }
-    return sum;
+    for (int col = threadIdx.x * 8; col < k.length; col += kClipThreads * 8) {
+        float x[8];
+        Values<F32>::load(v, col, k.length, x);
+        use(x, std::integral_constant<int, 8>{}, col);
+    }
+}
+
+template <bool F32>
+__device__ __forceinline__ double clip_squares(const void *grad, const ClipChunk &k)
+{
+    double sum[2] = {0.0, 0.0};
+    clip_each<F32>(grad, k, [&](const float (&x)[8], auto n, int) {
+#pragma unroll
+        for (int q = 0; q < decltype(n)::value; ++q) sum[q & 1] += (double)x[q] * (double)x[q];
+    });
+    return sum[0] + sum[1];
 }
 
 // the sum over the workgroup in thread 0, in a fixed order
@@ -76,7 +106,7 @@ __global__ __launch_bounds__(kClipThreads) void clip_squares_kernel(ClipTable t,
     const int chunks = t.first[t.n];
     for (int c = (int)blockIdx.x; c < chunks; c += (int)gridDim.x) {
         const ClipChunk k = clip_chunk(t, c);
-        sum += k.f32 ? clip_squares<true>(t.grad[k.tensor], k.at, k.length) : clip_squares<false>(t.grad[k.tensor], k.at, k.length);
+        sum += k.f32 ? clip_squares<true>(t.grad[k.tensor], k) : clip_squares<false>(t.grad[k.tensor], k);
     }
     sum = clip_sum<kClipThreads>(sum, part);
     if (threadIdx.x == 0) parts[blockIdx.x] = sum;
@@ -96,22 +126,27 @@ __global__ __launch_bounds__(1024) void clip_join_kernel(int64_t count, double *
     }
 }
 
-template <bool F32>
-__device__ __forceinline__ void clip_scale(const void *grad, void *out, int64_t at, int length, double factor)
+// PAST: past the caches, which then keep what is still to be read
+typedef lanes_u32x4 __attribute__((aligned(2))) ClipAny;
+template <bool F32, bool PAST>
+__device__ __forceinline__ void clip_scale(const void *grad, void *out, const ClipChunk &k, double factor)
 {
-    const auto *v = static_cast<const typename Values<F32>::T *>(grad) + at;
-    auto *o = static_cast<typename Values<F32>::T *>(out) + at;
-#pragma unroll 4
-    for (int col = threadIdx.x * 8; col < length; col += kClipThreads * 8) {
-        float x[8];
-        Values<F32>::load(v, col, length, x);
+    auto *o = static_cast<typename Values<F32>::T *>(out) + k.at;
+    clip_each<F32>(grad, k, [&](const float (&x)[8], auto n, int col) {
+        float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         // (in 64 bits: a factor below 2^-126 would lose bits as a float)
 #pragma unroll
-        for (int q = 0; q < 8; ++q) x[q] = (float)((double)x[q] * factor);
-        Values<F32>::store(o, col, length, x);
-    }
+        for (int q = 0; q < decltype(n)::value; ++q) y[q] = (float)((double)x[q] * factor);
+        lanes_u32x4 v;
+#pragma unroll
+        for (int q = 0; q < 4; ++q) v[q] = F32 ? __builtin_bit_cast(uint32_t, y[q]) : bf16_pair(y[2 * q], y[2 * q + 1]);
+        if (k.length != kChunk) Values<F32>::store(o, col, k.length, y);
+        else if constexpr (PAST) __builtin_nontemporal_store(v, reinterpret_cast<ClipAny *>(o + col));
+        else *reinterpret_cast<ClipAny *>(o + col) = v;
+    });
 }
 
+template <bool PAST>
 __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(ClipTable t, const double *at)
 {
     const double factor = *at;
@@ -120,8 +155,8 @@ __global__ __launch_bounds__(kClipThreads) void clip_scale_kernel(ClipTable t, c
         // from the end: what was read last is still in the caches
         const ClipChunk k = clip_chunk(t, chunks - 1 - i);
         if (factor == 1.0 && t.out[k.tensor] == t.grad[k.tensor]) continue;
-        if (k.f32) clip_scale<true>(t.grad[k.tensor], t.out[k.tensor], k.at, k.length, factor);
-        else clip_scale<false>(t.grad[k.tensor], t.out[k.tensor], k.at, k.length, factor);
+        if (k.f32) clip_scale<true, PAST>(t.grad[k.tensor], t.out[k.tensor], k, factor);
+        else clip_scale<false, PAST>(t.grad[k.tensor], t.out[k.tensor], k, factor);
     }
 }
 
@@ -185,8 +220,12 @@ hipError_t clip_launch(int n, const void *const *grads, const int64_t *counts, c
     });
     if (e == hipSuccess) e = launch_kernel(clip_join_kernel, dim3(1), dim3(1024), 0, st, all, parts, max_norm, norm);
     if (e != hipSuccess || !out) return e;
+    // Results that no cache would hold until they are read go past the caches (134 M floats: 292 us a call, so 275; from the first chunk on 307).
+    int64_t bytes = 0;
+    for (int i = 0; i < n; ++i) bytes += counts[i] > 0 ? counts[i] * (types[i] == POLYDL_F32 ? 4 : 2) : 0;
+    auto *scale = bytes > 192ll << 20 ? clip_scale_kernel<true> : clip_scale_kernel<false>;
     return each([&](const ClipTable &t, int blocks, double *) {
-        return launch_kernel(clip_scale_kernel, dim3((unsigned)blocks), dim3(kClipThreads), 0, st, t, (const double *)(parts + all));
+        return launch_kernel(scale, dim3((unsigned)blocks), dim3(kClipThreads), 0, st, t, (const double *)(parts + all));
     });
 }
 

@@ -17,13 +17,15 @@ template <int LANES>
 __device__ __forceinline__ float norm_sum(float x, float *part)
 {
     if constexpr (LANES <= 64) return group_sum<LANES>(x);
+    constexpr int kWaves = LANES / 64;
     x = wave_sum(x);
     __syncthreads();                       // the last sum has been read
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
     __syncthreads();
-    float sum = part[0];
+    const float *mine = part + threadIdx.x / LANES * kWaves;
+    float sum = mine[0];
 #pragma unroll
-    for (int w = 1; w < LANES / 64; ++w) sum += part[w];
+    for (int w = 1; w < kWaves; ++w) sum += mine[w];
     return sum;
 }
 
@@ -147,10 +149,194 @@ hipError_t norm_launch(const NormProblem &p, hipStream_t st)
 }
 
 // ---- gradient ---------------------------------------------------------------------------------------------------
-// dx: a workgroup a row, read twice.
-constexpr int kGradThreads = 256;
+// A workgroup goes over rows with a stride, LANES lanes a row; every lane keeps its columns' parts of dgamma and dbeta in registers from row to row, so x
+// and dy are read once for all three results, the next row while this one is worked on.  At its end the workgroup's rows meet in LDS in their order, the
+// workgroups' sums in the workspace.
+// Bound: HBM, x and dy read and dx written once (16384 x 2048 bfloat16: 36.3 us, and 4.2 for the workgroups' sums, 201 MB at 5.0 TB/s; in kernels of their own dx
+// took 41.7 us and the weights 22.4 more).
+constexpr int kGradThreads = 512, kGradBlocks = 256;         // (more workgroups write more sums: 16 KB each for rows of 2048)
+// Two sums over LANES neighbouring threads; more than a wave's meet in `part`, of which neighbouring rows use different halves, so that one barrier a row
+// suffices.
+template <int LANES>
+__device__ __forceinline__ void norm_sums(float &a, float &b, float (*part)[kGradThreads / 64], int row)
+{
+    a = group_sum<LANES < 64 ? LANES : 64>(a);
+    b = group_sum<LANES < 64 ? LANES : 64>(b);
+    if constexpr (LANES > 64) {
+        constexpr int kWaves = LANES / 64;
+        part += (row & 1) * 2;
+        if ((threadIdx.x & 63) == 0) {
+            part[0][threadIdx.x >> 6] = a;
+            part[1][threadIdx.x >> 6] = b;
+        }
+        __syncthreads();
+        const int mine = threadIdx.x / LANES * kWaves;
+        a = part[0][mine];
+        b = part[1][mine];
+#pragma unroll
+        for (int w = 1; w < kWaves; ++w) {
+            a += part[0][mine + w];
+            b += part[1][mine + w];
+        }
+    }
+}
+
+template <bool DY32, bool X32, int LANES, int NV, bool WEIGHTS>
+__global__ __launch_bounds__(kGradThreads) void norm_bwd_kernel(NormGradProblem p, float *parts)
+{
+    constexpr int kRows = kGradThreads / LANES, kColumns = LANES * NV * 8, kWaves = kGradThreads / 64;
+    constexpr int kTurns = LANES < 64 ? kWaves : kRows;      // groups of lanes that hold the same columns, after a wave's own have met
+    __shared__ float part[4][kWaves];
+    __shared__ float sums[WEIGHTS && kTurns > 1 ? kColumns : 1];
+    const int l = threadIdx.x % LANES, group = threadIdx.x / LANES;
+    const int64_t step = (int64_t)gridDim.x * kRows;
+    typename Values<X32>::Raw xr[NV];
+    typename Values<DY32>::Raw dr[NV];
+    float w[NV][8], dg[NV][8], db[NV][8], mean = 0.f, rstd = 0.f;
+    const auto load = [&](int64_t t) {
+        if (t >= p.T) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * LANES + l) * 8;
+            if (col >= p.D) continue;
+            xr[i] = Values<X32>::load_raw(static_cast<const typename Values<X32>::T *>(p.x) + t * p.ldx, col, p.D);
+            dr[i] = Values<DY32>::load_raw(static_cast<const typename Values<DY32>::T *>(p.dy) + t * p.lddy, col, p.D);
+        }
+        mean = p.mean[t];
+        rstd = p.rstd[t];
+    };
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int col = (i * LANES + l) * 8;
+#pragma unroll
+        for (int q = 0; q < 8; ++q) { w[i][q] = 1.f; dg[i][q] = db[i][q] = 0.f; }
+        xr[i] = {};
+        dr[i] = {};
+        if (p.gamma && col < p.D) Values<true>::load(p.gamma, col, p.D, w[i]);
+    }
+    // (all groups of a workgroup take the same number of turns, for its barriers)
+    int64_t t = (int64_t)blockIdx.x * kRows + group;
+    load(t);
+    const float over = 1.f / (float)p.D;
+    int row = 0;
+    for (int64_t t0 = (int64_t)blockIdx.x * kRows; t0 < p.T; t0 += step, t += step, ++row) {
+        float h[NV][8], g[NV][8], sum = 0.f, along = 0.f;
+        const float m = mean, s = rstd;
+        const bool here = t < p.T;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            Values<X32>::convert(xr[i], h[i]);
+            Values<DY32>::convert(dr[i], g[i]);
+        }
+        load(t + step);
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                const bool there = here && (i * LANES + l) * 8 + q < p.D;
+                h[i][q] = there ? (h[i][q] - m) * s : 0.f;
+                if constexpr (WEIGHTS) {
+                    dg[i][q] += there ? g[i][q] * h[i][q] : 0.f;
+                    db[i][q] += there ? g[i][q] : 0.f;
+                }
+                g[i][q] = there ? g[i][q] * w[i][q] : 0.f;
+                sum += g[i][q];
+                along += g[i][q] * h[i][q];
+            }
+        if (!p.dx) continue;
+        norm_sums<LANES>(sum, along, part, row);
+        sum *= over;
+        along *= over;
+        if (!here) continue;
+        auto *dx = static_cast<typename Values<X32>::T *>(p.dx) + t * p.lddx;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * LANES + l) * 8;
+            if (col >= p.D) continue;
+#pragma unroll
+            for (int q = 0; q < 8; ++q) g[i][q] = s * (g[i][q] - sum - h[i][q] * along);
+            Values<X32>::store(dx, col, p.D, g[i]);
+        }
+    }
+    if constexpr (!WEIGHTS) return;
+#pragma unroll
+    for (int x = LANES; x < 64; x += x)
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int q = 0; q < 8; ++q) {
+                dg[i][q] += __shfl_xor(dg[i][q], x);
+                db[i][q] += __shfl_xor(db[i][q], x);
+            }
+    const auto join = [&](float (&v)[NV][8], int which) {
+        // column col of the sums lies where a lane's eight are apart, so that neighbouring lanes fall on different banks
+        for (int turn = 0; turn < kTurns && kTurns > 1; ++turn) {
+            if (turn == (LANES < 64 ? (int)threadIdx.x >> 6 : group) && (LANES >= 64 || (threadIdx.x & 63) < LANES)) {
+#pragma unroll
+                for (int i = 0; i < NV; ++i)
+#pragma unroll
+                    for (int q = 0; q < 8; ++q) {
+                        float *at = &sums[(i * 8 + q) * LANES + l];
+                        v[i][q] = turn ? *at + v[i][q] : v[i][q];
+                        *at = v[i][q];
+                    }
+            }
+            __syncthreads();
+        }
+        const int last = kTurns - 1;
+        if ((LANES < 64 ? (int)threadIdx.x >> 6 : group) != last || (LANES < 64 && (threadIdx.x & 63) >= LANES)) return;
+        float *out = which ? p.dbeta : p.dgamma;
+        if (gridDim.x > 1) out = parts + ((int64_t)blockIdx.x * 2 + which) * p.D;
+        if (!out) return;
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * LANES + l) * 8;
+            if (col >= p.D) continue;
+            if (gridDim.x == 1 && p.accumulate) {
+                float was[8];
+                Values<true>::load(out, col, p.D, was);
+#pragma unroll
+                for (int q = 0; q < 8; ++q) v[i][q] += was[q];
+            }
+            Values<true>::store(out, col, p.D, v[i]);
+        }
+    };
+    join(dg, 0);
+    if (kTurns > 1) __syncthreads();
+    join(db, 1);
+}
+
+// The workgroups' sums: 64 columns of dgamma or dbeta a workgroup, every sixteenth part a wave, sixteen of them on their way at a time.
+__global__ __launch_bounds__(1024) void norm_join_kernel(int D, int chunks, const float *parts, float *dgamma, float *dbeta, int accumulate)
+{
+    __shared__ float sums[16][64];
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, which = (int)blockIdx.y;
+    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
+    float *out = which ? dbeta : dgamma;
+    if (!out) return;
+    constexpr int kHeld = 16;
+    float sum = 0.f;
+    for (int c0 = wave; c0 < chunks; c0 += 16 * kHeld) {
+        float v[kHeld];
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) {
+            const int c = c0 + i * 16;
+            v[i] = c < chunks && col < D ? parts[((int64_t)c * 2 + which) * D + col] : 0.f;
+        }
+#pragma unroll
+        for (int i = 0; i < kHeld; ++i) sum += v[i];
+    }
+    sums[wave][lane] = sum;
+    __syncthreads();
+    if (wave || col >= D) return;
+    for (int w = 1; w < 16; ++w) sum += sums[w][lane];
+    out[col] = accumulate ? out[col] + sum : sum;
+}
+
+// Rows too long for registers.  dx: a workgroup a row, read twice.
+constexpr int kLongThreads = 256;
 template <bool DY32, bool X32>
-__global__ __launch_bounds__(kGradThreads) void norm_dx_kernel(NormGradProblem p)
+__global__ __launch_bounds__(kLongThreads) void norm_dx_kernel(NormGradProblem p)
 {
     __shared__ float part[16];
     const int64_t t = block_number();
@@ -171,15 +357,15 @@ __global__ __launch_bounds__(kGradThreads) void norm_dx_kernel(NormGradProblem p
             h[q] = col + q < p.D ? (h[q] - mean) * rstd : 0.f;
         }
     };
-    for (int col = threadIdx.x * 8; col < p.D; col += kGradThreads * 8) {
+    for (int col = threadIdx.x * 8; col < p.D; col += kLongThreads * 8) {
         read(col);
 #pragma unroll
         for (int q = 0; q < 8; ++q) { sum += g[q]; along += g[q] * h[q]; }
     }
-    sum = norm_sum<kGradThreads>(sum, part) / (float)p.D;
-    along = norm_sum<kGradThreads>(along, part) / (float)p.D;
+    sum = norm_sum<kLongThreads>(sum, part) / (float)p.D;
+    along = norm_sum<kLongThreads>(along, part) / (float)p.D;
     auto *dx = static_cast<typename Values<X32>::T *>(p.dx) + t * p.lddx;
-    for (int col = threadIdx.x * 8; col < p.D; col += kGradThreads * 8) {
+    for (int col = threadIdx.x * 8; col < p.D; col += kLongThreads * 8) {
         read(col);
 #pragma unroll
         for (int q = 0; q < 8; ++q) g[q] = rstd * (g[q] - sum - h[q] * along);
@@ -229,45 +415,63 @@ __global__ __launch_bounds__(256) void norm_dweights_kernel(NormGradProblem p, i
     }
 }
 
-// The chunks' sums: 64 columns of dgamma or dbeta a workgroup, every sixteenth chunk a wave.
-__global__ __launch_bounds__(1024) void norm_join_kernel(int D, int chunks, const float *parts, float *dgamma, float *dbeta, int accumulate)
+constexpr int kGradLongest = kGradThreads * 16;              // values of a row that registers hold
+
+// Rows that a workgroup takes at a time.
+static int norm_rows(int D) { return D <= 16 * 8 ? kGradThreads / 16 : D <= 64 * 16 ? kGradThreads / 64 : D <= 128 * 16 ? kGradThreads / 128 : D <= 256 * 16 ? kGradThreads / 256 : 1; }
+static int norm_chunks(int T, int D)
 {
-    __shared__ float sums[16][64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, which = (int)blockIdx.y;
-    const int64_t col = (int64_t)blockIdx.x * 64 + lane;
-    float *out = which ? dbeta : dgamma;
-    if (!out) return;
-    float sum = 0.f;
-    if (col < D)
-        for (int c = wave; c < chunks; c += 16) sum += parts[((int64_t)c * 2 + which) * D + col];
-    sums[wave][lane] = sum;
-    __syncthreads();
-    if (wave || col >= D) return;
-    for (int w = 1; w < 16; ++w) sum += sums[w][lane];
-    out[col] = accumulate ? out[col] + sum : sum;
+    const int64_t rows = D <= kGradLongest ? norm_rows(D) : 64, chunks = ((int64_t)T + rows - 1) / rows;
+    return (int)(chunks < kGradBlocks ? chunks : kGradBlocks);
 }
 
-static int norm_chunks(int T) { return T <= 0 ? 0 : (int)(((int64_t)T + 63) / 64 < 256 ? ((int64_t)T + 63) / 64 : 256); }
+size_t norm_bwd_workspace_bytes(int T, int D) { return (size_t)norm_chunks(T, D) * 2 * (size_t)D * sizeof(float); }
 
-size_t norm_bwd_workspace_bytes(int T, int D) { return (size_t)norm_chunks(T) * 2 * (size_t)D * sizeof(float); }
-
-template <bool DY32, bool X32>
+template <bool DY32, bool X32, int LANES, int NV>
 static hipError_t norm_bwd_run(const NormGradProblem &p, float *parts, hipStream_t st)
 {
+    // without weights nothing is kept from row to row: more workgroups even the rows out
+    const int64_t rows = kGradThreads / LANES, all = ((int64_t)p.T + rows - 1) / rows;
+    if (!p.dgamma && !p.dbeta)
+        return launch_kernel((norm_bwd_kernel<DY32, X32, LANES, NV, false>), dim3((unsigned)(all < 2048 ? all : 2048)), dim3(kGradThreads), 0, st, p, parts);
+    const int chunks = norm_chunks(p.T, p.D);
+    const hipError_t e = launch_kernel((norm_bwd_kernel<DY32, X32, LANES, NV, true>), dim3((unsigned)chunks), dim3(kGradThreads), 0, st, p, parts);
+    if (e != hipSuccess || chunks == 1) return e;
+    return launch_kernel(norm_join_kernel, dim3((unsigned)((p.D + 63) / 64), 2u), dim3(1024), 0, st, p.D, chunks, parts, p.dgamma, p.dbeta, p.accumulate);
+}
+
+template <bool DY32, bool X32>
+static hipError_t norm_bwd_long(const NormGradProblem &p, float *parts, hipStream_t st)
+{
     hipError_t e = hipSuccess;
-    if (p.dx && p.T > 0) e = launch_kernel((norm_dx_kernel<DY32, X32>), many_blocks(p.T, kGradThreads), dim3(kGradThreads), 0, st, p);
+    if (p.dx) e = launch_kernel((norm_dx_kernel<DY32, X32>), many_blocks(p.T, kLongThreads), dim3(kLongThreads), 0, st, p);
     if (e != hipSuccess || (!p.dgamma && !p.dbeta)) return e;
-    const int chunks = norm_chunks(p.T), per = chunks ? (int)(((int64_t)p.T + chunks - 1) / chunks) : 0;
-    if (chunks) e = launch_kernel((norm_dweights_kernel<DY32, X32>), dim3((unsigned)chunks, (unsigned)((p.D + 511) / 512)), dim3(256), 0, st, p, per, parts);
+    const int chunks = norm_chunks(p.T, p.D), per = (int)(((int64_t)p.T + chunks - 1) / chunks);
+    e = launch_kernel((norm_dweights_kernel<DY32, X32>), dim3((unsigned)chunks, (unsigned)((p.D + 511) / 512)), dim3(256), 0, st, p, per, parts);
     if (e != hipSuccess) return e;
     return launch_kernel(norm_join_kernel, dim3((unsigned)((p.D + 63) / 64), 2u), dim3(1024), 0, st, p.D, chunks, parts, p.dgamma, p.dbeta, p.accumulate);
+}
+
+template <bool DY32, bool X32>
+static hipError_t norm_bwd_pick(const NormGradProblem &p, float *parts, hipStream_t st)
+{
+    if (p.T <= 0)                      // sums of nothing
+        return launch_kernel(norm_join_kernel, dim3((unsigned)((p.D + 63) / 64), 2u), dim3(1024), 0, st, p.D, 0, parts, p.dgamma, p.dbeta, p.accumulate);
+    if (p.D <= 16 * 8) return norm_bwd_run<DY32, X32, 16, 1>(p, parts, st);
+    if (p.D <= 64 * 8) return norm_bwd_run<DY32, X32, 64, 1>(p, parts, st);
+    if (p.D <= 64 * 16) return norm_bwd_run<DY32, X32, 64, 2>(p, parts, st);
+    // (four units a lane would not fit in its registers beside their sums)
+    if (p.D <= 128 * 16) return norm_bwd_run<DY32, X32, 128, 2>(p, parts, st);
+    if (p.D <= 256 * 16) return norm_bwd_run<DY32, X32, 256, 2>(p, parts, st);
+    if (p.D <= 512 * 16) return norm_bwd_run<DY32, X32, 512, 2>(p, parts, st);
+    return norm_bwd_long<DY32, X32>(p, parts, st);
 }
 
 hipError_t norm_bwd_launch(const NormGradProblem &p, void *workspace, hipStream_t st)
 {
     float *parts = static_cast<float *>(workspace);
-    if (p.dy_f32) return p.x_f32 ? norm_bwd_run<true, true>(p, parts, st) : norm_bwd_run<true, false>(p, parts, st);
-    return p.x_f32 ? norm_bwd_run<false, true>(p, parts, st) : norm_bwd_run<false, false>(p, parts, st);
+    if (p.dy_f32) return p.x_f32 ? norm_bwd_pick<true, true>(p, parts, st) : norm_bwd_pick<true, false>(p, parts, st);
+    return p.x_f32 ? norm_bwd_pick<false, true>(p, parts, st) : norm_bwd_pick<false, false>(p, parts, st);
 }
 
 }  // namespace polydl

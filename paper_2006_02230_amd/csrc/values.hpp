@@ -15,25 +15,45 @@ template <bool F32>
 struct Values {
     using T = std::conditional_t<F32, float, uint16_t>;
 
-    // Values col .. col + 7 of a row of `length`, zeros behind its end (col < length)
-    static __device__ __forceinline__ void load(const T *row, int col, int length, float (&v)[8])
+    // what a load gives, before it is waited for
+    struct Raw { std::conditional_t<F32, values_f32x4, lanes_u32x4> v[F32 ? 2 : 1]; };
+    static __device__ __forceinline__ Raw load_raw(const T *row, int col, int length)
     {
         const int n = length - col;
+        Raw r;
         if constexpr (F32) {
             const float *p = row + col;
             if (n >= 8) {
-                const values_f32x4 a = reinterpret_cast<const Floats4Any *>(p)[0].v, b = reinterpret_cast<const Floats4Any *>(p)[1].v;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { v[i] = a[i]; v[4 + i] = b[i]; }
+                r.v[0] = reinterpret_cast<const Floats4Any *>(p)[0].v;
+                r.v[1] = reinterpret_cast<const Floats4Any *>(p)[1].v;
             } else {
+                r.v[0] = r.v[1] = values_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                for (int i = 0; i < 8; ++i) v[i] = i < n ? p[i] : 0.f;
+                for (int i = 0; i < 7; ++i)
+                    if (i < n) r.v[i >> 2][i & 3] = p[i];
             }
         } else {
-            const lanes_u32x4 u = load_unit8(row + col, n, length);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) { v[2 * i] = bf16_lo(u[i]); v[2 * i + 1] = bf16_hi(u[i]); }
+            r.v[0] = load_unit8(row + col, n, length);
         }
+        return r;
+    }
+    static __device__ __forceinline__ void convert(const Raw &r, float (&v)[8])
+    {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            if constexpr (F32) {
+                v[i] = r.v[0][i];
+                v[4 + i] = r.v[1][i];
+            } else {
+                v[2 * i] = bf16_lo(r.v[0][i]);
+                v[2 * i + 1] = bf16_hi(r.v[0][i]);
+            }
+        }
+    }
+    // Values col .. col + 7 of a row of `length`, zeros behind its end (col < length)
+    static __device__ __forceinline__ void load(const T *row, int col, int length, float (&v)[8])
+    {
+        convert(load_raw(row, col, length), v);
     }
     static __device__ __forceinline__ void store(T *row, int col, int length, const float (&v)[8])
     {

@@ -34,15 +34,18 @@ def mx4_quantise(x, out=None, stream=None):
         _no_graph()
     dev, K = _device(), x.shape[-1]
     codes, scales = mx4_shapes(*x.shape)
-    if out is None:
-        out = Mx4(_new(codes, torch.uint8, x, stream), _new(scales, torch.uint8, x, stream))
     if x.dim() == 2:
         rows, (xp, ldx) = x.shape[0], _matrix(x, "x", x.dtype, x.shape, dev)
     else:
         rows, xp, ldx = x.shape[0] * x.shape[1], _dense(x, "x", x.dtype, x.shape, dev), K
-    _check(lib.polydl_mx4_quantise(rows, K, xp, ldx, _type(x.dtype), _dense(out[0], "q", torch.uint8, codes, dev),
-                                   _dense(out[1], "scales", torch.uint8, scales, dev), _stream_ptr(stream)), "polydl_mx4_quantise")
-    return Mx4(*out)
+    if out is None:
+        out = Mx4(_new(codes, torch.uint8, x, stream), _new(scales, torch.uint8, x, stream))
+        qp, sp = out.q.data_ptr(), out.scales.data_ptr()
+    else:
+        out = Mx4(*out)
+        qp, sp = _dense(out.q, "q", torch.uint8, codes, dev), _dense(out.scales, "scales", torch.uint8, scales, dev)
+    _check(lib.polydl_mx4_quantise(rows, K, xp, ldx, _type(x.dtype), qp, sp, _stream_ptr(stream)), "polydl_mx4_quantise")
+    return out
 
 
 def mx4_dequantise(x, K, out=None, out_dtype=torch.bfloat16, stream=None):

@@ -12,7 +12,7 @@ import ctypes
 import torch
 
 from .binding import _check, _new, _stream_ptr, lib
-from .experts import _TYPES, _dense, _device, _matrix, _no_graph, _type
+from .experts import _dense, _device, _matrix, _no_graph, _type
 
 _i, _p, _l, _z, _f, _d = ctypes.c_int, ctypes.c_void_p, ctypes.c_int64, ctypes.c_size_t, ctypes.c_float, ctypes.c_double
 for _name, _args in {
@@ -44,11 +44,13 @@ def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, out=None, out_dtype=None, 
     """polydl_layernorm_fwd on the rows of x [T][D] (float32 or bfloat16): Norm(y [T][D] of out_dtype (None: x's), mean [T], rstd [T])."""
     _lost(x, gamma, beta)
     (T, D), dev = x.shape, _device()
+    xp, ldx = _matrix(x, "x", x.dtype, (T, D), dev)
     if out is None:
         out = _new((T, D), x.dtype if out_dtype is None else out_dtype, x, stream)
+        yp, ldy = out.data_ptr(), D
+    else:
+        yp, ldy = _matrix(out, "out", out.dtype, (T, D), dev)
     mean, rstd = _new((2, T), torch.float32, x, stream).unbind(0)
-    xp, ldx = _matrix(x, "x", x.dtype, (T, D), dev)
-    yp, ldy = _matrix(out, "out", out.dtype, (T, D), dev)
     _check(lib.polydl_layernorm_fwd(T, D, xp, ldx, _type(x.dtype), _dense(gamma, "gamma", torch.float32, (D,), dev),
                                     _dense(beta, "beta", torch.float32, (D,), dev), eps, yp, ldy, _type(out.dtype), mean.data_ptr(), rstd.data_ptr(),
                                     _stream_ptr(stream)), "polydl_layernorm_fwd")
@@ -131,8 +133,6 @@ _Tensor = torch.Tensor
 # A check is one pass over the list: tensor by tensor, with calls for each, 300 tensors took 145 us.
 def _listed(tensors, name, dev):
     """The types, lengths and layouts (None: all contiguous) of a list of dense tensors, checked."""
-    if not all([isinstance(t, _Tensor) for t in tensors]):
-        raise TypeError("%s must be tensors" % name)
     types = [t.dtype for t in tensors]
     if not set(types) <= {torch.float32, torch.bfloat16}:
         raise TypeError("%s must be float32 or bfloat16 tensors" % name)
@@ -159,7 +159,7 @@ def _gradients(grads):
     if torch.is_grad_enabled() and any([t.requires_grad for t in grads]):
         _no_graph()
     n = len(grads)
-    return grads, types, counts, layouts, _addresses(grads), (_l * n)(*counts), (_i * n)(*[_TYPES[t] for t in types])
+    return grads, types, counts, layouts, _addresses(grads), (_l * n)(*counts), (_i * n)(*[t is torch.bfloat16 for t in types])
 
 
 def _norm_space(like, n, counts, stream):
