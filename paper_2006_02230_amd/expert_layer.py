@@ -1,5 +1,6 @@
 """A layer of experts from the library's operators: the router's product (sgemm), the choice and plan (route), two products grouped by
-expert with ReLU between them, the weighted sum, and all their gradients; answers from 4-bit weights.
+expert with ReLU between them, the weighted sum, and all their gradients, the router's balance loss among them; answers from 4-bit weights, as integers
+or in microscaled floating point.
 
     python -m paper_2006_02230_amd.expert_layer      # trains one on a synthetic map, then answers with its weights in 4 bits
 """
@@ -9,6 +10,8 @@ import torch
 
 from . import binding as B
 from . import experts as X
+from . import mx4 as M
+from . import training as Y
 
 Gradients = collections.namedtuple("Gradients", "x router w1 w2")
 
@@ -22,11 +25,14 @@ class ExpertLayer:
     """out[t] = sum over the k chosen experts e of weight[t][e] * w2[e] relu(w1[e] x[t]), weights softmax(x[t] router) over the chosen.
 
     router [D][E] float32, w1 [E][F][D] and w2 [E][D][F] bfloat16, x [T][D] bfloat16.  `forward` leaves what `backward` needs in `kept`;
-    with several forwards before their backwards, take it from there after each and give it to its backward."""
+    with several forwards before their backwards, take it from there after each and give it to its backward.
 
-    def __init__(self, router, w1, w2, k):
-        self.router, self.w1, self.w2, self.k = router, w1, w2, k
-        self.kept, self.waiting = None, 0
+    balance: how much of the router's balance loss belongs to the loss that is trained on.  Where it is not 0, a forward that keeps leaves the loss and the
+    choices' counts in `used` (training.Balance), and the gradients are those of the whole."""
+
+    def __init__(self, router, w1, w2, k, balance=0.0):
+        self.router, self.w1, self.w2, self.k, self.balance = router, w1, w2, k, balance
+        self.kept, self.waiting, self.used = None, 0, None
 
     def forward(self, x, keep=True):
         """out [T][D] bfloat16.  keep=False: an answer without a backward, of which nothing is kept."""
@@ -36,7 +42,8 @@ class ExpertLayer:
         h = X.grouped_gemm_bf16(x, self.w1, r.offsets, rows=r.tokens, act="relu")
         y = X.grouped_gemm_bf16(h, self.w2, r.offsets)
         if keep:
-            self.kept, self.waiting = (x, xf, logits, r, h, y), self.waiting + 1
+            self.used = Y.balance(logits, r.ids) if self.balance else None
+            self.kept, self.waiting = (x, xf, logits, r, h, y, self.used), self.waiting + 1
         return X.combine_bf16(y, r.slots, r.weights)
 
     def backward(self, dout, kept=None):
@@ -50,13 +57,15 @@ class ExpertLayer:
                                    "a backward" % self.waiting)
             kept = self.kept
         self.waiting = max(self.waiting - 1, 0)
-        x, xf, logits, r, h, y = kept
+        x, xf, logits, r, h, y, used = kept
         dy, dweights = X.combine_bwd_bf16(dout, y, r.slots, r.weights)
         dh = X.grouped_gemm_dx_bf16(dy, self.w2, r.offsets, h=h, act="relu")
         dw2 = X.grouped_gemm_dw_bf16(dy, h, r.offsets)
         dw1 = X.grouped_gemm_dw_bf16(dh, x, r.offsets, rows=r.tokens)
         dx = X.combine_bf16(X.grouped_gemm_dx_bf16(dh, self.w1, r.offsets, out_dtype=torch.bfloat16), r.slots, out_dtype=torch.float32)
         dlogits = X.route_bwd(logits, r.ids, r.weights, dweights)
+        if used is not None:
+            Y.balance_bwd(logits, used.counts, used.rows, self.balance, out=dlogits, accumulate=True)
         if not len(x):
             return Gradients(dx.bfloat16(), torch.zeros_like(self.router), dw1, dw2)
         drouter = B.sgemm(xf.t().contiguous(), dlogits, torch.empty_like(self.router), alpha=1.0, beta=0.0)
@@ -66,6 +75,10 @@ class ExpertLayer:
     def coded(self, group=128, asymmetric=False):
         """The same layer with its experts' weights in 4 bits."""
         return CodedExpertLayer(self, group, asymmetric)
+
+    def microscaled(self):
+        """The same layer with its experts' weights, and what they are multiplied with, in microscaled 4-bit floating point."""
+        return MicroscaledExpertLayer(self)
 
 
 class CodedExpertLayer:
@@ -81,6 +94,20 @@ class CodedExpertLayer:
         r = X.route(_logits(x.float(), self.router), self.k)
         h = X.w4_gemm_bf16(x, self.w1.q, self.w1.scales, F, self.group, zeros=self.w1.zeros, offsets=r.offsets, rows=r.tokens, act="relu")
         y = X.w4_gemm_bf16(h, self.w2.q, self.w2.scales, D, self.group, zeros=self.w2.zeros, offsets=r.offsets)
+        return X.combine_bf16(y, r.slots, r.weights)
+
+
+class MicroscaledExpertLayer:
+    """An ExpertLayer that answers: both operands of its products in microscaled 4-bit floating point, for one token and for whole prompts."""
+
+    def __init__(self, layer):
+        self.router, self.k = layer.router, layer.k
+        self.w1, self.w2 = M.mx4_quantise(layer.w1), M.mx4_quantise(layer.w2)
+
+    def forward(self, x):
+        r = X.route(_logits(x.float(), self.router), self.k)
+        h = M.mx4_gemm(M.mx4_quantise(x), self.w1, offsets=r.offsets, rows=r.tokens, act="relu")
+        y = M.mx4_gemm(M.mx4_quantise(h), self.w2, offsets=r.offsets)
         return X.combine_bf16(y, r.slots, r.weights)
 
 

@@ -1,0 +1,182 @@
+"""The operators around a layer of experts together, as a block that trains and answers: against 64 bits, captured, with several forwards, without tokens."""
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def L():
+    import torch
+    if not torch.cuda.is_available():
+        pytest.skip("no GPU")
+    from paper_2006_02230_amd import expert_block, expert_layer
+    return expert_block, expert_layer
+
+
+def gen(seed):
+    import torch
+    return torch.Generator(device="cuda").manual_seed(seed)
+
+
+def randn(g, *shape):
+    import torch
+    return torch.randn(*shape, generator=g, device="cuda")
+
+
+def make(L, g, D, F, E, k, balance):
+    layer = L[1].ExpertLayer(randn(g, D, E) * D ** -0.5, (randn(g, E, F, D) * D ** -0.5).bfloat16(), (randn(g, E, D, F) * F ** -0.5).bfloat16(), k, balance)
+    return L[0].ExpertBlock(1 + 0.2 * randn(g, D), 0.2 * randn(g, D), layer)
+
+
+def reference(block, x, ids):
+    """out and the leaves x, gamma, beta, router, w1, w2 in 64 bits, with the choices given.  The norm gives rows in bfloat16, and the layer's products are of
+    those: unrounded ones would open and close ReLUs whose sums lie within 2^-8 of their terms of zero, one in some 800, each of which changes its gradients
+    by all of them (0.03 of their norm)."""
+    import torch
+    layer = block.layer
+    leaves = [v.double().requires_grad_() for v in (x, block.gamma, block.beta, layer.router, layer.w1, layer.w2)]
+    X, G, B, R, W1, W2 = leaves
+    c = X - X.mean(1, keepdim=True)
+    n = c / torch.sqrt((c * c).mean(1, keepdim=True) + block.eps) * G + B
+    n = n + (block.kept[1].y.double() - n).detach()
+    logits = n @ R
+    p = torch.gather(logits, 1, ids).softmax(1)
+    out = X
+    for e in range(R.shape[1]):
+        there = ids == e
+        t = there.any(1).nonzero()[:, 0]
+        out = out.index_add(0, t, (p * there).sum(1)[t, None] * (torch.relu(n[t] @ W1[e].T) @ W2[e].T))
+    f = torch.bincount(ids.reshape(-1), minlength=R.shape[1]).double() / ids.numel()
+    return out, R.shape[1] * (f * logits.softmax(1).mean(0)).sum(), leaves
+
+
+@pytest.mark.parametrize("T,D,F,E,k,balance", [(1, 64, 128, 4, 2, 0.5), (100, 72, 88, 6, 3, 20.0), (700, 256, 512, 8, 2, 100.0), (700, 256, 512, 8, 2, 0.0)])
+def test_block_against_64_bits(L, T, D, F, E, k, balance):
+    g = gen(T + D)
+    block = make(L, g, D, F, E, k, balance)
+    x, dout = (2 * randn(g, T, D) + 0.5).bfloat16(), randn(g, T, D).bfloat16()
+    out = block.forward(x)
+    grads = block.backward(dout)
+    ids = block.layer.kept[3].ids.long()
+    want, loss, leaves = reference(block, x, ids)
+    ((want * dout.double()).sum() + balance * loss).backward()
+    if balance:
+        # the logits are products of rows rounded to bfloat16 (2^-8 of each), of size 1
+        assert abs(float(block.layer.used.loss) - float(loss.detach())) <= 2.0 ** -6 * float(loss.detach())
+    # roundings to bfloat16 on the way of a term, each of 2^-8 of it, independent, half more for unequal sizes: forward the normed row, the hidden one, the
+    # product, the weighted sum and the last sum; backward the five of what is multiplied with as far as it enters, and those of dy, dh, the rows' gradients
+    # through the products, the layer and the norm
+    for got, ref, n in [(out, want, 5)] + [(a, b.grad, 8) for a, b in zip(grads, leaves)]:
+        off = (got.double() - ref).norm() / ref.norm()
+        assert off <= 1.5 * n ** 0.5 * 2.0 ** -8, (float(off), n)
+
+
+def test_block_gradient_against_differences(L):
+    # along a direction of gamma and beta in float32; the forward's roundings to bfloat16 (five, 2^-8 of values near 1, independent over the T D outputs)
+    # over the step, and the step's own curvature by halving it
+    import torch
+    g = gen(3)
+    T, D = 512, 128
+    block = make(L, g, D, 256, 4, 4, 0.0)                  # all experts are chosen: no choice changes on the way
+    x, dout = randn(g, T, D).bfloat16(), randn(g, T, D).bfloat16()
+    block.forward(x)
+    grads = block.backward(dout)
+    dg, db = randn(g, D), randn(g, D)
+    want = float((grads.gamma * dg + grads.beta * db).sum())
+
+    def at(step):
+        moved = L[0].ExpertBlock(block.gamma + step * dg, block.beta + step * db, block.layer)
+        return float((moved.forward(x, keep=False).double() * dout.double()).sum())
+    slopes = [(at(s) - at(-s)) / (2 * s) for s in (0.25, 0.125)]
+    noise = 5 ** 0.5 * 2.0 ** -8 * float((dout.double() * x.double().abs().clamp(min=1)).norm()) / 0.25
+    assert abs(slopes[1] - want) <= 4 * noise + 2 * abs(slopes[0] - slopes[1]) + 0.02 * float(grads.gamma.norm() * dg.norm())
+
+
+def test_several_forwards_and_a_forward_that_keeps_nothing(L):
+    import torch
+    g = gen(5)
+    block = make(L, g, 64, 96, 4, 2, 0.1)
+    xs, dout = [randn(g, t, 64).bfloat16() for t in (30, 50)], [randn(g, t, 64).bfloat16() for t in (30, 50)]
+    want = []
+    for x, d in zip(xs, dout):
+        block.forward(x)
+        want.append(block.backward(d))
+    kept = []
+    for x in xs:
+        block.forward(x)
+        kept.append(block.kept)
+    with pytest.raises(RuntimeError, match="2 forwards wait"):
+        block.backward(dout[1])
+    block.forward(xs[0], keep=False)
+    for i in (1, 0):
+        for a, b in zip(block.backward(dout[i], kept[i]), want[i]):
+            assert torch.equal(a, b)
+    with pytest.raises(RuntimeError, match="needs a forward"):
+        make(L, g, 64, 96, 4, 2, 0.1).backward(dout[0])
+
+
+def test_block_without_tokens(L):
+    import torch
+    g = gen(6)
+    block = make(L, g, 64, 128, 4, 2, 0.1)
+    x = torch.empty(0, 64, dtype=torch.bfloat16, device="cuda")
+    assert block.forward(x).shape == (0, 64) and block.microscaled().forward(x).shape == (0, 64) and float(block.layer.used.loss) == 0
+    for got, like in zip(block.backward(x), (x, block.gamma, block.beta, block.layer.router, block.layer.w1, block.layer.w2)):
+        assert got.shape == like.shape and not bool(got.any())
+
+
+def test_captured_step(L):
+    # a training step's operators with the clipping of its gradients in one graph, replayed on other rows
+    import torch
+    from paper_2006_02230_amd import clip_grads
+    g = gen(7)
+    block = make(L, g, 128, 256, 8, 2, 0.5)
+    x, dout = randn(g, 300, 128).bfloat16(), randn(g, 300, 128).bfloat16()
+
+    def step():
+        out = block.forward(x)
+        grads = block.backward(dout)
+        return [out, block.layer.used.loss, clip_grads(grads[1:], 1.0), *grads]
+    step()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        held = step()
+    for seed in range(3):
+        x.copy_(randn(gen(seed), 300, 128))
+        dout.copy_(randn(gen(seed + 10), 300, 128))
+        graph.replay()
+        torch.cuda.synchronize()
+        for a, b in zip([t.clone() for t in held], step()):
+            assert torch.equal(a, b)
+        torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("T", [1, 40, 1500])
+def test_microscaled_answers(L, T):
+    """Against the same block with values that are exact in 4 bits: the weights, and the rows through an identity norm."""
+    import torch
+    from paper_2006_02230_amd import mx4_dequantise, mx4_quantise
+    g = gen(T)
+    block = make(L, g, 256, 512, 8, 2, 0.0)
+    layer = block.layer
+    small = layer.microscaled()
+    x = randn(g, T, 256).bfloat16()
+    got = small.forward(x)
+    # the layer in bfloat16 with the values that the codes stand for, the hidden rows converted on their way, too
+    from paper_2006_02230_amd import combine_bf16, grouped_gemm_bf16, route
+    w1, w2 = mx4_dequantise(small.w1, 256), mx4_dequantise(small.w2, 512)
+    r = route(L[1]._logits(x.float(), layer.router), layer.k)
+    h = grouped_gemm_bf16(mx4_dequantise(mx4_quantise(x), 256), w1, r.offsets, rows=r.tokens, act="relu")
+    y = grouped_gemm_bf16(mx4_dequantise(mx4_quantise(h), 512), w2, r.offsets)
+    want = combine_bf16(y, r.slots, r.weights)
+    # the same products of the same values, rounded to bfloat16: a sum near a border may round the other way (2^-8 of it), and then a code of the hidden row
+    # may, too (a quarter of it, in few places)
+    off = (got.double() - want.double()).norm() / want.double().norm()
+    assert off <= 2.0 ** -6, float(off)
+
+
+def test_block_trains_and_answers(L):
+    import math
+    losses, balances, norms, coded = L[0].main(steps=5, T=300, D=64, F=96, E=4)
+    assert len(losses) == 5 and all(map(math.isfinite, losses + balances + norms + [coded])) and all(b > 0 for b in balances)
