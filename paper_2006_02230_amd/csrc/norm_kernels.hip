@@ -443,13 +443,14 @@ static hipError_t norm_bwd_run(const NormGradProblem &p, float *parts, hipStream
 template <bool DY32, bool X32>
 static hipError_t norm_bwd_long(const NormGradProblem &p, float *parts, hipStream_t st)
 {
-    hipError_t e = hipSuccess;
-    if (p.dx) e = launch_kernel((norm_dx_kernel<DY32, X32>), many_blocks(p.T, kLongThreads), dim3(kLongThreads), 0, st, p);
-    if (e != hipSuccess || (!p.dgamma && !p.dbeta)) return e;
-    const int chunks = norm_chunks(p.T, p.D), per = (int)(((int64_t)p.T + chunks - 1) / chunks);
-    e = launch_kernel((norm_dweights_kernel<DY32, X32>), dim3((unsigned)chunks, (unsigned)((p.D + 511) / 512)), dim3(256), 0, st, p, per, parts);
-    if (e != hipSuccess) return e;
-    return launch_kernel(norm_join_kernel, dim3((unsigned)((p.D + 63) / 64), 2u), dim3(1024), 0, st, p.D, chunks, parts, p.dgamma, p.dbeta, p.accumulate);
+    if (p.dgamma || p.dbeta) {
+        const int chunks = norm_chunks(p.T, p.D), per = (int)(((int64_t)p.T + chunks - 1) / chunks);
+        hipError_t e = launch_kernel((norm_dweights_kernel<DY32, X32>), dim3((unsigned)chunks, (unsigned)((p.D + 511) / 512)), dim3(256), 0, st, p, per, parts);
+        if (e == hipSuccess)
+            e = launch_kernel(norm_join_kernel, dim3((unsigned)((p.D + 63) / 64), 2u), dim3(1024), 0, st, p.D, chunks, parts, p.dgamma, p.dbeta, p.accumulate);
+        if (e != hipSuccess) return e;
+    }
+    return p.dx ? launch_kernel((norm_dx_kernel<DY32, X32>), many_blocks(p.T, kLongThreads), dim3(kLongThreads), 0, st, p) : hipSuccess;
 }
 
 template <bool DY32, bool X32>

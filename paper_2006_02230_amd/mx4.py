@@ -5,6 +5,7 @@ grouped by expert (same names as the C entry points, argument marshalling only).
 caller makes `stream` wait for the arguments, keeps them until it has read them, and waits for it before using the results elsewhere."""
 import collections
 import ctypes
+import math
 
 import torch
 
@@ -29,7 +30,7 @@ def mx4_shapes(*shape):
 
 
 def mx4_quantise(x, out=None, stream=None):
-    """polydl_mx4_quantise: Mx4(q, scales) of x [rows][K] (any row stride) or [E][rows][K] (contiguous), float32 or bfloat16."""
+    """polydl_mx4_quantise: Mx4(q, scales) of x [rows][K] (any row stride) or [...][K] (contiguous), float32 or bfloat16."""
     if x.requires_grad:
         _no_graph()
     dev, K = _device(), x.shape[-1]
@@ -37,7 +38,7 @@ def mx4_quantise(x, out=None, stream=None):
     if x.dim() == 2:
         rows, (xp, ldx) = x.shape[0], _matrix(x, "x", x.dtype, x.shape, dev)
     else:
-        rows, xp, ldx = x.shape[0] * x.shape[1], _dense(x, "x", x.dtype, x.shape, dev), K
+        rows, xp, ldx = math.prod(x.shape[:-1]), _dense(x, "x", x.dtype, x.shape, dev), K
     if out is None:
         out = Mx4(_new(codes, torch.uint8, x, stream), _new(scales, torch.uint8, x, stream))
         qp, sp = out.q.data_ptr(), out.scales.data_ptr()
@@ -49,7 +50,7 @@ def mx4_quantise(x, out=None, stream=None):
 
 
 def mx4_dequantise(x, K, out=None, out_dtype=torch.bfloat16, stream=None):
-    """polydl_mx4_dequantise: the values [rows][K] or [E][rows][K] of Mx4(q, scales)."""
+    """polydl_mx4_dequantise: the values [...][K] of Mx4(q, scales)."""
     q, scales = x
     dev, lead = _device(), tuple(q.shape[:-1])
     codes, per_block = mx4_shapes(*lead, K)
@@ -58,7 +59,7 @@ def mx4_dequantise(x, K, out=None, out_dtype=torch.bfloat16, stream=None):
     if len(lead) == 1:
         rows, (yp, ldy) = lead[0], _matrix(out, "out", out.dtype, (*lead, K), dev)
     else:
-        rows, yp, ldy = lead[0] * lead[1], _dense(out, "out", out.dtype, (*lead, K), dev), K
+        rows, yp, ldy = math.prod(lead), _dense(out, "out", out.dtype, (*lead, K), dev), K
     _check(lib.polydl_mx4_dequantise(rows, K, _dense(q, "q", torch.uint8, codes, dev), _dense(scales, "scales", torch.uint8, per_block, dev), yp, ldy,
                                      _type(out.dtype), _stream_ptr(stream)), "polydl_mx4_dequantise")
     return out

@@ -117,6 +117,13 @@ def test_conversion_strides(P, name):
     three = P.mx4_quantise(x.reshape(3, 3, 131).contiguous())
     assert torch.equal(three.q.reshape(9, -1), q.q) and torch.equal(three.scales.reshape(9, -1), q.scales)
     assert torch.equal(P.mx4_dequantise(three, 131).reshape(9, 131), P.mx4_dequantise(q, 131))
+    four = P.mx4_quantise(x.reshape(3, 1, 3, 131).contiguous())
+    assert torch.equal(four.q.reshape(9, -1), q.q) and torch.equal(P.mx4_dequantise(four, 131).reshape(9, 131), P.mx4_dequantise(q, 131))
+    one = P.mx4_quantise(x[4].contiguous())
+    assert torch.equal(one.q, q.q[4]) and torch.equal(one.scales, q.scales[4]) and torch.equal(P.mx4_dequantise(one, 131), P.mx4_dequantise(q, 131)[4])
+    for shape in ((0, 131), (2, 0, 131)):
+        none = P.mx4_quantise(torch.empty(shape, device="cuda"))
+        assert P.mx4_dequantise(none, 131).shape == shape
     given = P.Mx4(torch.zeros_like(q.q), torch.zeros_like(q.scales))
     assert P.mx4_quantise(x, out=given).q is given.q and torch.equal(given.q, q.q)
 
