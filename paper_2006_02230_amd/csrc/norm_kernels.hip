@@ -187,7 +187,7 @@ __global__ __launch_bounds__(kGradThreads) void norm_bwd_kernel(NormGradProblem 
     constexpr int kRows = kGradThreads / LANES, kColumns = LANES * NV * 8, kWaves = kGradThreads / 64;
     constexpr int kTurns = LANES < 64 ? kWaves : kRows;      // groups of lanes that hold the same columns, after a wave's own have met
     __shared__ float part[4][kWaves];
-    __shared__ float sums[WEIGHTS && kTurns > 1 ? kColumns : 1];
+    __shared__ float sums[WEIGHTS && kTurns > 1 ? kTurns / 2 * 2 * kColumns : 1];
     const int l = threadIdx.x % LANES, group = threadIdx.x / LANES;
     const int64_t step = (int64_t)gridDim.x * kRows;
     typename Values<X32>::Raw xr[NV];
@@ -268,24 +268,36 @@ __global__ __launch_bounds__(kGradThreads) void norm_bwd_kernel(NormGradProblem 
                 dg[i][q] += __shfl_xor(dg[i][q], x);
                 db[i][q] += __shfl_xor(db[i][q], x);
             }
-    const auto join = [&](float (&v)[NV][8], int which) {
-        // column col of the sums lies where a lane's eight are apart, so that neighbouring lanes fall on different banks
-        for (int turn = 0; turn < kTurns && kTurns > 1; ++turn) {
-            if (turn == (LANES < 64 ? (int)threadIdx.x >> 6 : group) && (LANES >= 64 || (threadIdx.x & 63) < LANES)) {
+    // Half of the groups hand their sums to the other half, until one has them all (in turns, eight groups took 1 us longer).  What a lane hands over lies LANES
+    // apart, so that neighbouring lanes fall on different banks.
+    const int mine = LANES < 64 ? (int)threadIdx.x >> 6 : group;
+    const bool speaks = LANES >= 64 || (int)(threadIdx.x & 63) < LANES;
+    for (int half = kTurns / 2; half >= 1; half >>= 1) {
+        if (speaks && mine >= half && mine < 2 * half) {
+            float *to = sums + (mine - half) * 2 * kColumns + l;
 #pragma unroll
-                for (int i = 0; i < NV; ++i)
+            for (int i = 0; i < NV; ++i)
 #pragma unroll
-                    for (int q = 0; q < 8; ++q) {
-                        float *at = &sums[(i * 8 + q) * LANES + l];
-                        v[i][q] = turn ? *at + v[i][q] : v[i][q];
-                        *at = v[i][q];
-                    }
-            }
-            __syncthreads();
+                for (int q = 0; q < 8; ++q) {
+                    to[(i * 8 + q) * LANES] = dg[i][q];
+                    to[kColumns + (i * 8 + q) * LANES] = db[i][q];
+                }
         }
-        const int last = kTurns - 1;
-        if ((LANES < 64 ? (int)threadIdx.x >> 6 : group) != last || (LANES < 64 && (threadIdx.x & 63) >= LANES)) return;
-        float *out = which ? p.dbeta : p.dgamma;
+        __syncthreads();
+        if (speaks && mine < half) {
+            const float *from = sums + mine * 2 * kColumns + l;
+#pragma unroll
+            for (int i = 0; i < NV; ++i)
+#pragma unroll
+                for (int q = 0; q < 8; ++q) {
+                    dg[i][q] += from[(i * 8 + q) * LANES];
+                    db[i][q] += from[kColumns + (i * 8 + q) * LANES];
+                }
+        }
+        __syncthreads();
+    }
+    if (mine != 0 || !speaks) return;
+    const auto leave = [&](float (&v)[NV][8], float *out, int which) {
         if (gridDim.x > 1) out = parts + ((int64_t)blockIdx.x * 2 + which) * p.D;
         if (!out) return;
 #pragma unroll
@@ -301,9 +313,8 @@ __global__ __launch_bounds__(kGradThreads) void norm_bwd_kernel(NormGradProblem 
             Values<true>::store(out, col, p.D, v[i]);
         }
     };
-    join(dg, 0);
-    if (kTurns > 1) __syncthreads();
-    join(db, 1);
+    leave(dg, p.dgamma, 0);
+    leave(db, p.dbeta, 1);
 }
 
 // The workgroups' sums: 64 columns of dgamma or dbeta a workgroup, every sixteenth part a wave, sixteen of them on their way at a time.
