@@ -208,7 +208,7 @@ static hipError_t mx4_few_run(const Mx4Problem &p, hipStream_t st)
 // ---- tiles ------------------------------------------------------------------------------------------------------
 // A workgroup owns tiles of BM rows by BN columns, one after another, and walks the reduction in stages of 256 inputs, 128 bytes of codes a row,
 // BUFFERS of them in LDS; a wave keeps a tile WM x WN in registers.  Codes lie in LDS as they lie in memory, the unit (block) c of a row in
-// place c ^ ((row >> 1) & 7), so that 16 neighbouring rows' units fall on different banks.  An instruction j of the stage's four takes the blocks j and
+// place c ^ ((row >> 1) & 7), so that 16 neighbouring rows' units fall on different banks (row & 7: nearly twice the conflicts).  An instruction j of the stage's four takes the blocks j and
 // 4 + j, one a half wave: a lane's four scales of a stage are then one word, of which the instruction picks byte j.
 // Loads go from memory into LDS without registers; lanes without a row, or past the end of theirs, use an offset out of the
 // descriptor's range, which reads as zero.  Scales come 16 bytes a row, for two stages: a load of 4 bytes fetches as many cache lines (8192 x 8192 x
@@ -249,7 +249,7 @@ __global__ __launch_bounds__(T::kThreads) void mx4_tile_kernel(Mx4Problem p, int
     struct Out { int rows, cols; int64_t at; };
     const auto turn = [](int r) { return (r >> 1) & 7; };
 
-    // Sets up tile `id` for loading.  Where there is none its loads are of zeros, and false is returned.
+    // Sets up tile `id` for loading; where there is none its loads are of zeros.  Returns whether there is one.
     const auto find = [&](int id, Out &out) {
         GroupTile t;
         const bool there = tiles.find(id, &t);
@@ -310,12 +310,11 @@ __global__ __launch_bounds__(T::kThreads) void mx4_tile_kernel(Mx4Problem p, int
             }
         }
     };
-    // A stage is fetched in kLoads loads after begin(): the rows' (A), then the columns' (B), which late() keeps while the next stage is set up.
-    // A thread's units lie in the same place of their rows, so they all are behind the rows' end or none is.
+    // A stage is fetched in kLoads loads after begin().  A thread's units lie in the same place of their rows, so they all are behind the rows' end or none is.
     const int unit_of = (tid & 7) ^ turn(tid >> 3);
     static_assert(T::kThreads / 8 % 16 == 0, "turn()");
-    gg_i32x4 rsrc_a, rsrc_b, late_rsrc;
-    uint32_t far = 0, late_off[T::kUnitsB];
+    gg_i32x4 rsrc_a, rsrc_b;
+    uint32_t far = 0;
     const auto begin = [&](int s) {
         rsrc_a = gg_rsrc(base_a, (int64_t)kFarRecords);
         rsrc_b = gg_rsrc(base_b, (int64_t)kFarRecords);
@@ -323,28 +322,18 @@ __global__ __launch_bounds__(T::kThreads) void mx4_tile_kernel(Mx4Problem p, int
         base_b += kMx4Stage * 16;
         far = s * kMx4Stage + unit_of < p.KB ? 0u : kFarOffset;
     };
-    const auto late = [&]() {
-        late_rsrc = rsrc_b;
-#pragma unroll
-        for (int i = 0; i < T::kUnitsB; ++i) late_off[i] = off_b[i] | far;
-    };
     // g counts the stages from the first tile on
-    const auto load_a = [&](uint32_t g, int i) {
-        gg_dma(rsrc_a, lds0 + g % kBuffers * T::kStageBytes + (uint32_t)(i * T::kThreads + wave * 64) * 16u, off_a[i] | far);
+    const auto load = [&](uint32_t g, int i) {
+        const uint32_t at = lds0 + g % kBuffers * T::kStageBytes;
+        if (i < T::kUnitsA) gg_dma(rsrc_a, at + (uint32_t)(i * T::kThreads + wave * 64) * 16u, off_a[i] | far);
+        else gg_dma(rsrc_b, at + BM * 128u + (uint32_t)((i - T::kUnitsA) * T::kThreads + wave * 64) * 16u, off_b[i - T::kUnitsA] | far);
     };
-    const auto load_b = [&](uint32_t g, int i) {
-        gg_dma(late_rsrc, lds0 + g % kBuffers * T::kStageBytes + BM * 128u + (uint32_t)(i * T::kThreads + wave * 64) * 16u, late_off[i]);
-    };
-    const auto load_all_a = [&](uint32_t g) {
+    const auto load_all = [&](uint32_t g) {
 #pragma unroll
-        for (int i = 0; i < T::kUnitsA; ++i) load_a(g, i);
-    };
-    const auto load_all_b = [&](uint32_t g) {
-#pragma unroll
-        for (int i = 0; i < T::kUnitsB; ++i) load_b(g, i);
+        for (int i = 0; i < T::kLoads; ++i) load(g, i);
     };
     // Waits until this wave's loads are down to those of BEHIND stages (scales not counted: they come before their stage) and what it has stored since, then
-    // for the other waves.
+    // for the other waves.  Loads and global (not flat) stores are counted and end in their order, as the compiler's own waits take them to.
     const auto land = [&](auto behind, auto stores) {
         asm volatile("" ::: "memory");
         gg_wait<decltype(behind)::value * T::kLoads + decltype(stores)::value>();
@@ -379,14 +368,13 @@ __global__ __launch_bounds__(T::kThreads) void mx4_tile_kernel(Mx4Problem p, int
     mx4_f32x16 acc[MI][NI];
     lanes_u32x4 a0[MI], b0[NI], a1[MI], b1[NI];              // operands of an instruction and of the next one
     uint32_t as[2][MI], bs[2][NI];                           // scales of a stage and of the next one
-    // Instruction j of stage g, and meanwhile the reads for the one after it.  The last of a stage also asks for the rows of the stage that takes its
-    // buffer, the first one of the next stage for the columns (a tile's first stage has had them): all of them at once hold the waves up (8192 x 8192 x
-    // 8192: 248 us).
+    // Instruction j of stage g, and meanwhile the reads for the one after it; the last of a stage also asks for the stage that takes its buffer, between all
+    // its products (between the first two of them: 2 % slower).
     // next: the number of stage g+1 in its tile.
     const auto step = [&](uint32_t g, int next, auto which, auto odd, auto first, auto stores, const lanes_u32x4 (&a)[MI], const lanes_u32x4 (&b)[NI],
                           lanes_u32x4 (&a_next)[MI], lanes_u32x4 (&b_next)[NI]) {
         constexpr int J = decltype(which)::value, kOdd = decltype(odd)::value;
-        constexpr bool kLast = J == 3, kColumns = J == 0 && !decltype(first)::value;
+        constexpr bool kLast = J == 3;
         if constexpr (kLast) land(std::integral_constant<int, kBuffers - 2>{}, stores);      // stage g+1; and this wave has what it read of stage g
         constexpr int kReads = MI + NI, kAll = MI * NI;
         const uint32_t scales = kLast ? scales_at(g + 1, next) : 0u, there = kLast ? there_of(next) : 0u;
@@ -403,11 +391,7 @@ __global__ __launch_bounds__(T::kThreads) void mx4_tile_kernel(Mx4Problem p, int
                 }
                 if constexpr (kLast) {
 #pragma unroll
-                    for (int r = at * T::kUnitsA / kAll; r < (at + 1) * T::kUnitsA / kAll; ++r) load_a(g + kBuffers, r);
-                }
-                if constexpr (kColumns) {
-#pragma unroll
-                    for (int r = at * T::kUnitsB / kAll; r < (at + 1) * T::kUnitsB / kAll; ++r) load_b(g + kBuffers - 1, r);
+                    for (int r = at * T::kLoads / kAll; r < (at + 1) * T::kLoads / kAll; ++r) load(g + kBuffers, r);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -520,9 +504,7 @@ __global__ __launch_bounds__(T::kThreads) void mx4_tile_kernel(Mx4Problem p, int
     for (int g = 0; g < kBuffers; ++g) {
         if (g & 1) advance((uint32_t)g, no);
         else advance((uint32_t)g, yes);
-        late();
-        load_all_a((uint32_t)g);
-        load_all_b((uint32_t)g);
+        load_all((uint32_t)g);
     }
     land(none, none);
     first_reads(0u, 0, none);
@@ -536,36 +518,31 @@ __global__ __launch_bounds__(T::kThreads) void mx4_tile_kernel(Mx4Problem p, int
         step(g, next_stage, std::integral_constant<int, 3>{}, odd, no, stores, a1, b1, a0, b0);
     };
     // a stage without products: a wave whose part of the tile does not exist takes part in the loads, and so does every wave in a stage of zeros
-    const auto pass = [&](int next_stage, auto next_odd, bool first) {
-        if (!first) load_all_b(g + kBuffers - 1);
+    const auto pass = [&](int next_stage, auto next_odd) {
         land(std::integral_constant<int, kBuffers - 2>{}, none);
-        load_all_a(g + kBuffers);
+        load_all(g + kBuffers);
         first_reads(g + 1, next_stage, next_odd);
     };
     while (true) {
         const bool busy = wave_value((int)(wm < now.rows && wn < now.cols));
         for (int s = 0; s < padded; s += 2) {
             // (Here, where the loop branches anyway: at a branch between them the compiler gathers the matrix instructions on one side of it.)
-            late();
             if (at == padded) {                              // the tile is loaded: on to the next one
                 at = 0;
                 id += (int)gridDim.x;
                 more = find(id, next);
             }
             advance(g + kBuffers, yes);
-            if (!busy || s >= stages) pass(s + 1, odd, s == 0);
+            if (!busy || s >= stages) pass(s + 1, odd);
             else if (s == 0) stage(1, even, yes, std::integral_constant<int, kStores>{});
             else stage(s + 1, even, no, none);
             ++g;
-            late();
             advance(g + kBuffers, no);
             const int after = s + 2 == padded ? 0 : s + 2;
-            if (!busy || s + 1 >= stages) pass(after, even, false);
+            if (!busy || s + 1 >= stages) pass(after, even);
             else stage(after, odd, no, none);
             ++g;
         }
-        late();
-        load_all_b(g + kBuffers - 1);                        // before the results leave: the wait for them does not wait for those
         leave(now);
         if (!more) break;
         now = next;
