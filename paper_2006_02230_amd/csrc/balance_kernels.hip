@@ -212,17 +212,21 @@ __global__ __launch_bounds__(1024) void balance_join_kernel(BalanceArgs a)
     balance_finish<1024>(a.p, sums[0], counts[0], rows, part);
 }
 
-// Rows of a workgroup at least, and workgroups at most: a row a group of lanes, four times; one workgroup adds the others' sums up.
-constexpr int kBalanceRows = 256, kBalanceBlocks = 128;
-static int balance_blocks(int T)
+// One workgroup takes up to 256 rows (a second launch costs as much as four rounds of rows); more rows go to workgroups of one round, or of two where a wave takes a
+// row, but at most 256, or 128: one workgroup adds their sums up (16384 x 128: 13.7 us with 128 or 256 workgroups, 17.7 with 64; 100000 x 128: 41, 31 and 69; 8192 x 1000: 43
+// and 49 with 128 and 256; 300 x 1000 16 us, with 64 rows a workgroup 29).
+constexpr int kBalanceRows = 256;
+static int balance_blocks(int T, int E)
 {
-    const int64_t blocks = T <= kBalanceRows ? 1 : ((int64_t)T + 63) / 64;
-    return (int)(blocks < kBalanceBlocks ? blocks : kBalanceBlocks);
+    const bool wide = E > 256;
+    const int64_t rows = wide ? 16 : 64, blocks = T <= (wide ? 16 : kBalanceRows) ? 1 : ((int64_t)T + rows - 1) / rows;
+    const int64_t most = wide ? 128 : 256;
+    return (int)(blocks < most ? blocks : most);
 }
 
 size_t balance_workspace_bytes(int T, int E)
 {
-    const size_t blocks = (size_t)balance_blocks(T);
+    const size_t blocks = (size_t)balance_blocks(T, E);
     return blocks <= 1 ? 0 : blocks * ((size_t)E * 8 + 4);
 }
 
@@ -236,7 +240,7 @@ static hipError_t balance_run(const BalanceArgs &a, hipStream_t st)
 
 hipError_t balance_launch(const BalanceProblem &p, void *workspace, hipStream_t st)
 {
-    BalanceArgs a{p, balance_blocks(p.T), 0, nullptr, nullptr};
+    BalanceArgs a{p, balance_blocks(p.T, p.E), 0, nullptr, nullptr};
     a.per = (int)(((int64_t)p.T + a.blocks - 1) / a.blocks);
     if (a.blocks > 1) {
         a.part = static_cast<float *>(workspace);

@@ -65,17 +65,19 @@ def layernorm_bwd(dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=Non
         raise ValueError("weights=False forms neither dgamma nor dbeta")
     if accumulate and (dgamma is None or dbeta is None):
         raise ValueError("accumulate needs dgamma and dbeta")
-    if dx is None:
-        dx = _new((T, D), x.dtype, x, stream)
-    if weights and dgamma is None:
-        dgamma = _new((D,), torch.float32, x, stream)
-    if weights and dbeta is None:
-        dbeta = _new((D,), torch.float32, x, stream)
-    need = lib.polydl_layernorm_bwd_workspace_bytes(T, D) if weights else 0
-    space = _new((need,), torch.uint8, x, stream) if need else None
     dp, lddy = _matrix(dy, "dy", dy.dtype, (T, D), dev)
     xp, ldx = _matrix(x, "x", x.dtype, (T, D), dev)
-    op, lddx = _matrix(dx, "dx", x.dtype, (T, D), dev)
+    if dx is None:
+        dx = _new((T, D), x.dtype, x, stream)
+        op, lddx = dx.data_ptr(), D
+    else:
+        op, lddx = _matrix(dx, "dx", x.dtype, (T, D), dev)
+    if weights and dgamma is None and dbeta is None:
+        dgamma, dbeta = _new((2, D), torch.float32, x, stream).unbind(0)          # an allocation takes longer than a view
+    elif weights:
+        dgamma, dbeta = (_new((D,), torch.float32, x, stream) if t is None else t for t in (dgamma, dbeta))
+    need = lib.polydl_layernorm_bwd_workspace_bytes(T, D) if weights else 0
+    space = _new((need,), torch.uint8, x, stream) if need else None
     _check(lib.polydl_layernorm_bwd(T, D, dp, lddy, _type(dy.dtype), xp, ldx, _type(x.dtype), _dense(mean, "mean", torch.float32, (T,), dev),
                                     _dense(rstd, "rstd", torch.float32, (T,), dev), _dense(gamma, "gamma", torch.float32, (D,), dev), op, lddx,
                                     _dense(dgamma, "dgamma", torch.float32, (D,), dev), _dense(dbeta, "dbeta", torch.float32, (D,), dev),
