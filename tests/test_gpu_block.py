@@ -291,6 +291,22 @@ def test_balance_gradient(P, T, E, k):
     assert (np.abs(host(half) * 2 * float(dloss) - want) <= tol + 4 * u * np.abs(want)).all()
 
 
+@pytest.mark.parametrize("T,E,scale", [(5, 8, 1), (300, 6, 1), (70, 300, 1 << 20)])
+def test_balance_gradient_of_even_use(P, T, E, scale):
+    # evenly used experts: no gradient, not what roundings leave of one; and with one choice more each for a few, all of its digits
+    import torch
+    x = randn(gen(E), T, E)
+    rows = torch.tensor(T, dtype=torch.int32, device="cuda")
+    counts = torch.full((E,), 40 * scale, dtype=torch.int32, device="cuda")
+    assert not P.balance_bwd(x, counts, rows).any()
+    counts[::3] += 1
+    got, p = host(P.balance_bwd(x, counts, rows)), ob.probabilities(host(x))[0]
+    f = host(counts) / host(counts).sum() - 1 / E
+    # p's own error, a sum of E, five products
+    tol = (rel_p(host(x), E) * 2 + (E / 16 + 32) * u) * E / T * p * (np.abs(f) + (p @ np.abs(f))[:, None])
+    assert (np.abs(got - ob.balance_bwd(host(x), counts.cpu().numpy(), T)) <= tol + 1e-15 * p * E / T).all()
+
+
 def test_balance_without_rows_or_choices(P):
     import torch
     empty = P.balance(torch.empty(0, 6, device="cuda"), torch.empty(0, 2, dtype=torch.int32, device="cuda"))
