@@ -371,7 +371,8 @@ int polydl_balance_bwd(int T, int E, const float *logits, const int32_t *counts,
  * polydl_grad_norm: *norm = sqrt of the sum of all squares, summed in 64 bits, so that no square overflows; 0 without values.
  * polydl_clip_grads: and out[i] = grads[i] * min(1, max_norm / norm), of types[i]; out NULL: in place.  A norm that is not finite
  * (an infinity or NaN among the values) changes no value, nor does one of max_norm or less: in place nothing is written then.  *norm is
- * the norm before, and tells.  max_norm >= 0.  A tensor that is written must not overlap another one, read or written, except its own grads[i]
+ * the norm before, and tells; one past the largest float is finite in the 64 bits that it is formed in, so the values are scaled, and is given
+ * as infinity.  max_norm >= 0.  A tensor that is written must not overlap another one, read or written, except its own grads[i]
  * exactly (POLYDL_ERR_UNSUPPORTED): a tensor that is listed twice would be scaled twice.  Empty tensors may be NULL.
  * workspace: polydl_clip_workspace_bytes(n, counts) bytes, 8-byte aligned, contents undefined afterwards. */
 size_t polydl_clip_workspace_bytes(int n, const int64_t *counts);

@@ -18,7 +18,7 @@ int type_bytes(int type) { return type == POLYDL_F32 ? 4 : 2; }
 bool aligned_type(const void *p, int type) { return aligned(p, type_bytes(type)); }
 // lengths whose last tile stays within the kernels' 32-bit arithmetic; strides and counts whose byte offsets 64 bits hold with room to spare
 constexpr int kMaxLength = 0x7fff0000, kMaxRow = 1 << 24;
-constexpr int64_t kMaxRowStride = 1ll << 40, kMaxElements = 1ll << 60;
+constexpr int64_t kMaxRowStride = 1ll << 40, kMaxElements = 1ll << 60, kMaxValues = 1ll << 42;
 bool too_many(int64_t a, int64_t b, int64_t c) { return (__int128)a * b * c >= kMaxElements; }
 
 // hipErrorInvalidValue from a launcher here: no kernel holds the problem
@@ -31,7 +31,7 @@ int clip_check(int n, const void *const *grads, const int64_t *counts, const int
     for (int i = 0; i < n; ++i) {
         if (counts[i] < 0) return POLYDL_ERR_BAD_DIMENSION;
         if (counts[i] > 0 && !grads[i]) return POLYDL_ERR_NULL_POINTER;
-        if (!any_type(types[i]) || counts[i] > (1ll << 42)) return POLYDL_ERR_UNSUPPORTED;
+        if (!any_type(types[i]) || counts[i] > kMaxValues) return POLYDL_ERR_UNSUPPORTED;
         if (!aligned_type(grads[i], types[i])) return POLYDL_ERR_UNSUPPORTED;
     }
     return aligned(norm, 4) ? POLYDL_OK : POLYDL_ERR_UNSUPPORTED;
@@ -153,7 +153,13 @@ int polydl_balance_bwd(int T, int E, const float *logits, const int32_t *counts,
     return launched(balance_bwd_launch(T, E, logits, counts, rows, coefficient, dloss, dlogits, accumulate != 0, (hipStream_t)stream));
 }
 
-size_t polydl_clip_workspace_bytes(int n, const int64_t *counts) { return n < 0 || (n > 0 && !counts) ? 0 : clip_workspace_bytes(n, counts); }
+size_t polydl_clip_workspace_bytes(int n, const int64_t *counts)
+{
+    if (n < 0 || (n > 0 && !counts)) return 0;
+    for (int i = 0; i < n; ++i)
+        if (counts[i] < 0 || counts[i] > kMaxValues) return 0;
+    return clip_workspace_bytes(n, counts);
+}
 
 int polydl_grad_norm(int n, const void *const *grads, const int64_t *counts, const int *types, float *norm, void *workspace,
                      size_t workspace_bytes, void *stream)

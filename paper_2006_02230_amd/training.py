@@ -135,7 +135,7 @@ _Tensor = torch.Tensor
 # A check is one pass over the list: tensor by tensor, with calls for each, 300 tensors took 145 us.
 def _listed(tensors, name, dev):
     """The types, lengths and layouts (None: all contiguous) of a list of dense tensors, checked."""
-    types = [t.dtype for t in tensors]
+    types = [getattr(t, "dtype", None) for t in tensors]
     if not set(types) <= {torch.float32, torch.bfloat16}:
         raise TypeError("%s must be float32 or bfloat16 tensors" % name)
     if set(map(_Tensor.get_device, tensors)) - {dev} or dev is None:
@@ -179,8 +179,8 @@ def grad_norm(grads, stream=None):
 
 def clip_grads(grads, max_norm, out=None, stream=None):
     """polydl_clip_grads: scales a list of tensors to a norm of at most max_norm, in place or into the tensors of `out` (of the same types and
-    lengths, and where they are not contiguous of the same shapes and strides); returns the norm [] (float32) before.  Where that is not finite,
-    nothing is scaled."""
+    lengths, and where they are not contiguous of the same shapes and strides); returns the norm [] (float32) before.  Where an infinity or NaN is
+    among the values, nothing is scaled."""
     grads, kinds, lengths, layouts, at, counts, types = _gradients(grads)
     to = None
     if out is not None:

@@ -154,3 +154,18 @@ def test_binding_refusals():
     for t, filled in ((torch.empty(3, 4, 5).permute(2, 0, 1), True), (torch.empty(3, 4)[:, :2], False), (torch.empty(1, 4).expand(3, 4), False),
                       (torch.empty(5, 1, 3)[:, :, :1], False), (torch.empty(4, 3).t(), True)):
         assert P.training._filled(t) == filled
+
+
+def test_clip_workspace_of_refused_lengths():
+    import numpy as np
+    for bad in (-1, (1 << 42) + 1, (1 << 63) - 1):
+        counts = np.array([5, bad], dtype=np.int64)
+        assert P.lib.polydl_clip_workspace_bytes(2, counts.ctypes.data) == 0
+
+
+def test_clip_refuses_what_is_no_tensor():
+    import numpy as np
+    for bad in (None, 1.0, np.zeros(3, dtype=np.float32)):
+        for call in (lambda: P.grad_norm([bad]), lambda: P.clip_grads([bad], 1.0)):
+            with pytest.raises(TypeError):
+                call()
