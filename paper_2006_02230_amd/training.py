@@ -6,6 +6,7 @@ any row stride; their columns are contiguous.
 
 `stream` (None: torch's current stream) is where a call runs.  What it allocates is that stream's memory; as with any work on several streams, the
 caller makes `stream` wait for the arguments, keeps them until it has read them, and waits for it before using the results elsewhere."""
+import array
 import collections
 import ctypes
 
@@ -148,8 +149,13 @@ def _listed(tensors, name, dev):
     return types, list(map(_Tensor.numel, tensors)), layouts
 
 
+# (a ctypes array from a list takes four times as long as one of `array`)
 def _addresses(tensors):
-    return (_p * len(tensors))(*map(_Tensor.data_ptr, tensors))
+    return array.array("q", list(map(_Tensor.data_ptr, tensors)))
+
+
+def _at(values):
+    return values.buffer_info()[0]
 
 
 def _gradients(grads):
@@ -160,12 +166,12 @@ def _gradients(grads):
     types, counts, layouts = _listed(grads, "grads", _device())
     if torch.is_grad_enabled() and any([t.requires_grad for t in grads]):
         _no_graph()
-    n = len(grads)
-    return grads, types, counts, layouts, _addresses(grads), (_l * n)(*counts), (_i * n)(*[t is torch.bfloat16 for t in types])
+    half = torch.bfloat16
+    return grads, types, counts, layouts, _addresses(grads), array.array("q", counts), array.array("i", [t is half for t in types])
 
 
 def _norm_space(like, n, counts, stream):
-    need = lib.polydl_clip_workspace_bytes(n, counts)
+    need = lib.polydl_clip_workspace_bytes(n, _at(counts))
     return _new((), torch.float32, like, stream), _new((need,), torch.uint8, like, stream), need
 
 
@@ -173,7 +179,7 @@ def grad_norm(grads, stream=None):
     """polydl_grad_norm: the norm [] (float32) of a list of tensors (float32 or bfloat16, dense) taken as one vector."""
     grads, _, _, _, at, counts, types = _gradients(grads)
     norm, space, need = _norm_space(grads[0], len(grads), counts, stream)
-    _check(lib.polydl_grad_norm(len(grads), at, counts, types, norm.data_ptr(), space.data_ptr(), need, _stream_ptr(stream)), "polydl_grad_norm")
+    _check(lib.polydl_grad_norm(len(grads), _at(at), _at(counts), _at(types), norm.data_ptr(), space.data_ptr(), need, _stream_ptr(stream)), "polydl_grad_norm")
     return norm
 
 
@@ -189,6 +195,6 @@ def clip_grads(grads, max_norm, out=None, stream=None):
             raise ValueError("out must be tensors of the gradients' types, lengths and layouts")
         to = _addresses(out)
     norm, space, need = _norm_space(grads[0], len(grads), counts, stream)
-    _check(lib.polydl_clip_grads(len(grads), at, counts, types, float(max_norm), to, norm.data_ptr(), space.data_ptr(), need, _stream_ptr(stream)),
-           "polydl_clip_grads")
+    _check(lib.polydl_clip_grads(len(grads), _at(at), _at(counts), _at(types), float(max_norm), None if to is None else _at(to), norm.data_ptr(),
+                                 space.data_ptr(), need, _stream_ptr(stream)), "polydl_clip_grads")
     return norm
