@@ -67,9 +67,12 @@ def mx4_dequantise(x, K, out=None, out_dtype=torch.bfloat16, stream=None):
 
 def mx4_gemm(x, w, offsets=None, rows=None, act=None, out=None, out_dtype=torch.bfloat16, stream=None):
     """polydl_mx4_gemm: act(x[rows] @ w[e].T) for the rows of each group e, x an Mx4 of [x_rows][K] and w one of [E][N][K] or [N][K]; without
-    offsets all rows are one group."""
+    offsets all rows are one group.  Rows are filled up to 128 inputs, as mx4_shapes says."""
     (xq, xs), (wq, ws), dev = x, w, _device()
     E, N, width = wq.shape if wq.dim() == 3 else (1, *wq.shape)
+    # (the C call takes K and fills rows up to whole 128 inputs: shorter ones would be read with the stride of longer ones)
+    if width % 64:
+        raise ValueError("w.q must have rows of whole 64 bytes (mx4_shapes: filled up to 128 inputs), not of %d" % width)
     x_rows, blocks = xq.shape[0], width // 16
     if offsets is None and E > 1:
         raise ValueError("more than one matrix needs offsets")

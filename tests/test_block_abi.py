@@ -169,3 +169,14 @@ def test_clip_refuses_what_is_no_tensor():
         for call in (lambda: P.grad_norm([bad]), lambda: P.clip_grads([bad], 1.0)):
             with pytest.raises(TypeError):
                 call()
+
+
+def test_mx4_product_refuses_rows_that_are_not_filled_up():
+    # rows of 1, 2, 3, 5, 6, 7 blocks, or of no whole block, of x and w alike: the library's rows are whole fours of blocks, and it would read the next ones'
+    import torch
+    zeros = lambda *s: torch.zeros(s, dtype=torch.uint8)                  # noqa: E731
+    for width in (1, 16, 32, 48, 63, 65, 80, 96, 112, 1040):
+        x, w = P.Mx4(zeros(4, width), zeros(4, width // 16)), P.Mx4(zeros(6, width), zeros(6, width // 16))
+        for call in (lambda: P.mx4_gemm(x, w), lambda: P.mx4_gemm(x, P.Mx4(w.q[None], w.scales[None]), offsets=torch.zeros(2, dtype=torch.int32))):
+            with pytest.raises(ValueError, match="128"):
+                call()

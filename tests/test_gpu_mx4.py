@@ -232,6 +232,22 @@ def test_product_of_one_matrix(P):
     assert P.mx4_gemm(P.Mx4(x.q[:0], x.scales[:0]), w).shape == (0, 50)
 
 
+def test_product_refuses_rows_that_are_not_filled_up(P):
+    # refused before a kernel that would read past them; the same codes filled up are taken
+    import torch
+    g = gen(9)
+    for M, N, K in ((1, 40, 32), (20, 70, 96), (300, 300, 160)):
+        x, w = P.mx4_quantise(randn(g, M, K)), P.mx4_quantise(randn(g, N, K))
+        short = [P.Mx4(t.q[:, :K // 2].contiguous(), t.scales[:, :K // 32].contiguous()) for t in (x, w)]
+        with pytest.raises(ValueError, match="128"):
+            P.mx4_gemm(*short)
+        for a, b in ((x, short[1]), (short[0], w)):
+            with pytest.raises(ValueError):
+                P.mx4_gemm(a, b)
+        want, m = product(values(P, x, K), values(P, w, K)[None], None, None, None, N)
+        check(P.mx4_gemm(x, w, out_dtype=torch.float32), want, m, K, "f32")
+
+
 @pytest.mark.parametrize("E,M", [(3, 40), (2, 700), (4, 5)])
 def test_product_plans_that_are_none(P, E, M):
     # offsets past the end, that go backwards or are negative: the nearest plan; no row is read or written elsewhere
