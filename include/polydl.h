@@ -336,11 +336,13 @@ int polydl_w4_gemm_bf16(int E, int M, int N, int K, int group, const int32_t *of
 
 /* Layer norm of the rows of x [T][D]: mean_t = sum_j x_tj / D, rstd_t = 1 / sqrt(sum_j (x_tj - mean_t)^2 / D + eps),
  * y_tj = (x_tj - mean_t) * rstd_t * gamma_j + beta_j.  x of x_type, y of y_type (polydl_type), gamma and beta D floats or NULL (ones, zeros).
- * mean and rstd (T floats each) are what the gradient needs; each may be NULL.  eps >= 0.  A row of equal values with eps = 0 has an
- * infinite rstd, and NaN where the formula has 0 * infinity.
+ * mean and rstd (T floats each) are what the gradient needs; each may be NULL.  eps >= 0.  A row of equal values gives y = beta, with eps = 0 an
+ * infinite rstd, and NaN where the formula has 0 * infinity.  y is formed from the mean before it is rounded to a float, so a mean of many times the row's
+ * spread costs none of its bits.  The squares are summed as floats: where their sum passes the largest one (values from about 2^60 on) rstd is 0.
  * polydl_layernorm_bwd: from dy [T][D] (dy_type), with h = (x - mean) * rstd and g = dy * gamma,
  *   dx_tj = rstd_t * (g_tj - sum_i g_ti / D - h_tj * sum_i g_ti h_ti / D), of x_type;
  *   dgamma_j = sum_t dy_tj h_tj, dbeta_j = sum_t dy_tj, float32; accumulate != 0 adds to what they hold.
+ * (h is formed from the mean that is given, a float: one of 2^b times the row's spread leaves h 24 - b bits.)
  * Each of dx, dgamma and dbeta may be NULL and is not formed then.  workspace: polydl_layernorm_bwd_workspace_bytes(T, D) bytes, 4-byte
  * aligned, contents undefined afterwards; not looked at where neither dgamma nor dbeta is asked for.  T = 0 gives dgamma and dbeta of zeros.
  * D <= 2^24.  Rows (ldx, ldy, lddy, lddx elements apart) may be longer than D. */

@@ -1,9 +1,14 @@
 // Layer norm of rows and its gradient.
 //
 // Forward: LANES lanes take a row and hold it in registers, NV units of eight values each, so it is read once; the mean first, then the squares of what
-// is left (no difference of large sums), then the result.  Longer rows are read three times, the second and third time from the L2.
+// is left (no difference of large sums), then the result.  A float32 sum's mean is off by an ulp or more of itself, which may be more than the row's
+// spread; the differences from it are nearly exact, and their own mean is what it is off by: that is taken out before the squares (16384 x 2048
+// bfloat16 31.0 -> 31.3 us in a graph, one row 3.7 -> 3.9).  Equal values leave zeros: their sums are off by some tens of ulps, so all differences are the same
+// few ulps, whose sum over 16384 values 24 bits hold exactly.  Longer rows are read three times, the second and third time from the L2, and
+// their mean is formed in 64 bits, which hold the sum of 2^24 equal floats exactly, too (1600 x 20480 bfloat16 43.6 -> 45.8 us).
 // Bound: HBM, x read and y written once.
 #include <hip/hip_runtime.h>
+#include <math.h>
 #include "block.hpp"
 #include "blocks.hpp"
 #include "internal.hpp"
@@ -29,6 +34,33 @@ __device__ __forceinline__ float norm_sum(float x, float *part)
     return sum;
 }
 
+// the sum over a workgroup of 64-bit values, in all of its threads, in a fixed order
+template <int THREADS>
+__device__ __forceinline__ double norm_sum(double x, double *part)
+{
+#pragma unroll
+    for (int n = 1; n < 64; n += n) x += __shfl_xor(x, n);
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = x;
+    __syncthreads();
+    double sum = part[0];
+#pragma unroll
+    for (int w = 1; w < THREADS / 64; ++w) sum += part[w];
+    return sum;
+}
+
+// a * b, rounded: what is subtracted from all values of a row and added to their mean again has to be one number, not a product fused into each
+__device__ __forceinline__ float norm_product(float a, float b)
+{
+#pragma clang fp contract(off)
+    return a * b;
+}
+// sum / n from n's reciprocal, exact where the quotient is a float: the first quotient's remainder is formed exactly and divided, too
+__device__ __forceinline__ float norm_quotient(float sum, float n, float over)
+{
+    const float q = norm_product(sum, over);
+    return fmaf(fmaf(-q, n, sum), over, q);
+}
+
 template <bool X32, bool Y32, int LANES, int NV>
 __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormProblem p)
 {
@@ -39,6 +71,7 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormPro
     if (LANES >= 64 && t >= p.T) return;               // (the same for a wave)
     const bool here = t < p.T;
     const auto *x = static_cast<const typename Values<X32>::T *>(p.x) + t * p.ldx;
+    const float length = (float)p.D, over = 1.f / length;      // (the quotients of the sums would wait for one another)
     float v[NV][8], sum = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i) {
@@ -49,16 +82,26 @@ __global__ __launch_bounds__(LANES > 256 ? LANES : 256) void norm_kernel(NormPro
     }
 #pragma unroll
     for (int i = 0; i < NV; ++i) sum += ((v[i][0] + v[i][1]) + (v[i][2] + v[i][3])) + ((v[i][4] + v[i][5]) + (v[i][6] + v[i][7]));
-    const float mean = norm_sum<LANES>(sum, part) / (float)p.D;
+    const float near = norm_product(norm_sum<LANES>(sum, part), over);
+    float left = 0.f;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+        for (int q = 0; q < 8; ++q) {
+            v[i][q] = (i * LANES + l) * 8 + q < p.D ? v[i][q] - near : 0.f;
+            left += v[i][q];
+        }
+    left = norm_quotient(norm_sum<LANES>(left, part), length, over);
+    const float mean = fabsf(left) < INFINITY ? near + left : near;      // (a row with an infinity has an infinite mean)
     float square = 0.f;
 #pragma unroll
     for (int i = 0; i < NV; ++i)
 #pragma unroll
         for (int q = 0; q < 8; ++q) {
-            v[i][q] = (i * LANES + l) * 8 + q < p.D ? v[i][q] - mean : 0.f;
+            v[i][q] = (i * LANES + l) * 8 + q < p.D ? v[i][q] - left : 0.f;
             square += v[i][q] * v[i][q];
         }
-    const float rstd = 1.f / sqrtf(norm_sum<LANES>(square, part) / (float)p.D + p.eps);
+    const float rstd = 1.f / sqrtf(norm_sum<LANES>(square, part) * over + p.eps);
     if (!here) return;
     if (l == 0) {
         if (p.mean) p.mean[t] = mean;
@@ -86,26 +129,31 @@ template <bool X32, bool Y32>
 __global__ __launch_bounds__(kNormLong) void norm_long_kernel(NormProblem p)
 {
     __shared__ float part[16];
+    __shared__ double wide[16];
     const int64_t t = block_number();
     if (t >= p.T) return;
     const auto *x = static_cast<const typename Values<X32>::T *>(p.x) + t * p.ldx;
-    float v[8], sum = 0.f;
+    float v[8];
+    double sum = 0.0;
     for (int col = threadIdx.x * 8; col < p.D; col += kNormLong * 8) {
         Values<X32>::load(x, col, p.D, v);
-        sum += ((v[0] + v[1]) + (v[2] + v[3])) + ((v[4] + v[5]) + (v[6] + v[7]));
+        sum += (((double)v[0] + v[1]) + ((double)v[2] + v[3])) + (((double)v[4] + v[5]) + ((double)v[6] + v[7]));
     }
-    const float mean = norm_sum<kNormLong>(sum, part) / (float)p.D;
+    const double mean = norm_sum<kNormLong>(sum, wide) / (double)p.D;
     float square = 0.f;
     for (int col = threadIdx.x * 8; col < p.D; col += kNormLong * 8) {
         Values<X32>::load(x, col, p.D, v);
         float s = 0.f;
 #pragma unroll
-        for (int q = 0; q < 8; ++q) s += col + q < p.D ? (v[q] - mean) * (v[q] - mean) : 0.f;
+        for (int q = 0; q < 8; ++q) {
+            const float c = (float)(v[q] - mean);
+            s += col + q < p.D ? c * c : 0.f;
+        }
         square += s;
     }
     const float rstd = 1.f / sqrtf(norm_sum<kNormLong>(square, part) / (float)p.D + p.eps);
     if (threadIdx.x == 0) {
-        if (p.mean) p.mean[t] = mean;
+        if (p.mean) p.mean[t] = (float)mean;
         if (p.rstd) p.rstd[t] = rstd;
     }
     auto *y = static_cast<typename Values<Y32>::T *>(p.y) + t * p.ldy;
@@ -117,7 +165,7 @@ __global__ __launch_bounds__(kNormLong) void norm_long_kernel(NormProblem p)
         if (p.gamma) Values<true>::load(p.gamma, col, p.D, g);
         if (p.beta) Values<true>::load(p.beta, col, p.D, b);
 #pragma unroll
-        for (int q = 0; q < 8; ++q) v[q] = (v[q] - mean) * rstd * g[q] + b[q];
+        for (int q = 0; q < 8; ++q) v[q] = (float)(v[q] - mean) * rstd * g[q] + b[q];
         Values<Y32>::store(y, col, p.D, v);
     }
 }

@@ -125,6 +125,49 @@ def test_layernorm_of_a_large_mean_keeps_the_variance(P, D):
         assert (np.abs(host(a) - b) <= tol).all()
 
 
+def centred_bounds(x, gamma, beta, eps, want, y_name):
+    """Bounds where the mean's own rounding must not reach y.  Whatever a first mean is off by, e <= (adds(D) + 2) u mean|x|, is among the values that it
+    leaves, and so in their mean, which is formed of |c| + e and taken out: a centred value is off by (adds(D) + 3) u (mean|c| + e) for all alike and by two
+    roundings of its own.  The variance, rstd and y follow as in norm_bounds; the mean is rounded once."""
+    D = x.shape[1]
+    y, mean, rstd = want
+    e = (adds(D) + 2) * u * np.abs(x).mean(1)
+    c = np.abs(x - mean[:, None])
+    var = (c * c).mean(1)
+    dc = (adds(D) + 3) * u * (c.mean(1) + e)
+    rel = 0.5 * ((adds(D) + 10) * u * var + 2 * dc ** 2) / (var + eps) + 4 * u
+    g = np.abs(gamma)
+    dy = g * rstd[:, None] * (dc[:, None] + c * (rel[:, None] + 7 * u)) + 2 * u * (np.abs(beta) + np.abs(y))
+    return dy + half_step(y_name) * (np.abs(y) + dy), u * np.abs(mean) + dc, rstd * rel
+
+
+@pytest.mark.parametrize("D", [100, 128, 500, 1000, 2000, 3000, 7000, 12288, 16384, 20001, 70001])
+@pytest.mark.parametrize("mean", [0.3, 4096.0, -50000.3, 1e6])
+def test_layernorm_of_a_large_mean(P, D, mean):
+    # a mean of up to a million times the spread; and rows whose first value, or one in the middle, is far larger than the others
+    g = gen(D)
+    x = randn(g, 5, D) + mean
+    x[3, 0], x[4, D // 2] = 3e4, -3e4
+    gamma, beta = 1 + 0.2 * randn(g, D), 0.3 * randn(g, D)
+    want = ob.layernorm(host(x), host(gamma), host(beta))
+    got = P.layernorm_fwd(x, gamma, beta)
+    for a, b, tol in zip(got, want, centred_bounds(host(x), host(gamma), host(beta), 1e-5, want, "f32")):
+        assert (np.abs(host(a) - b) <= tol).all(), (np.abs(host(a) - b) / tol).max()
+
+
+@pytest.mark.parametrize("D", [1, 3, 100, 300, 1000, 1999, 3000, 4097, 12288, 16383, 20001, 300001])
+@pytest.mark.parametrize("name", ["f32", "bf16"])
+def test_layernorm_of_equal_values_whose_sums_round(P, D, name):
+    import torch
+    x = torch.tensor([[0.1], [1000.7], [-4097.3], [50000.3], [1e-30], [3e30]], device="cuda").to(kind(name)).expand(6, D).contiguous()
+    beta = randn(gen(D), D)
+    f = P.layernorm_fwd(x, beta=beta, out_dtype=torch.float32)
+    assert torch.equal(f.mean, x[:, 0].float()) and torch.equal(f.y, beta.expand(6, D))
+    assert (np.abs(host(f.rstd) * 1e-5 ** 0.5 - 1) <= 4 * u).all()                # eps, rounded, its root and quotient
+    none = P.layernorm_fwd(x, eps=0.0)
+    assert bool(torch.isinf(none.rstd).all()) and bool(torch.isnan(none.y).all()) and torch.equal(none.mean, f.mean)
+
+
 @pytest.mark.parametrize("D", [50, 600, 2500, 17000])
 def test_broken_rows_stay_alone(P, D):
     import torch
