@@ -126,6 +126,16 @@ __global__ __launch_bounds__(1024) void clip_join_kernel(int64_t count, double *
     }
 }
 
+// A 64-bit value as the float that is rounded to the bfloat16 next to it: cut off, the last bit set where something was, so that it lies on no middle of two
+// bfloat16 values that the value itself does not lie on (134 M bfloat16 values: 130 us a call, rounded twice, so 134).
+__device__ __forceinline__ float clip_odd(double x)
+{
+    const float f = (float)x;
+    uint32_t u = __builtin_bit_cast(uint32_t, f);
+    if ((double)f != x) u = (u - (fabs((double)f) > fabs(x) ? 1u : 0u)) | 1u;      // (a NaN stays one)
+    return __builtin_bit_cast(float, u);
+}
+
 // PAST: past the caches, which then keep what is still to be read
 typedef lanes_u32x4 __attribute__((aligned(2))) ClipAny;
 template <bool F32, bool PAST>
@@ -136,7 +146,7 @@ __device__ __forceinline__ void clip_scale(const void *grad, void *out, const Cl
         float y[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
         // (in 64 bits: a factor below 2^-126 would lose bits as a float)
 #pragma unroll
-        for (int q = 0; q < decltype(n)::value; ++q) y[q] = (float)((double)x[q] * factor);
+        for (int q = 0; q < decltype(n)::value; ++q) y[q] = F32 ? (float)((double)x[q] * factor) : clip_odd((double)x[q] * factor);
         lanes_u32x4 v;
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = F32 ? __builtin_bit_cast(uint32_t, y[q]) : bf16_pair(y[2 * q], y[2 * q + 1]);

@@ -423,6 +423,41 @@ def test_clipping(P, case, ratio, in_place):
             assert np.array_equal(host(o), b)
 
 
+def nearest_bf16(w):
+    """64-bit values to the nearest bfloat16 ones, ties to even."""
+    step = np.exp2(np.maximum(np.frexp(w)[1] - 1, -126) - 7.0)
+    return np.round(w / step) * step
+
+
+@pytest.mark.parametrize("n", [3, 8192, 20000])
+@pytest.mark.parametrize("scale", [0, -100, -126, -130])
+def test_clipping_rounds_once(P, n, scale):
+    # products just beside the middle of two bfloat16 values, nearer to it than a float32 value is: one that is rounded to float32 on its way falls on the
+    # middle, and then on the even side of it.  Down to values below the normal ones, whose steps are equal.
+    import torch
+    wrong = 0
+    for i in range(12):
+        x = (1.5 + (2 * i + 1) / 128) * 2.0 ** scale
+        x = float(nearest_bf16(np.array([x]))[0])
+        low = nearest_bf16(np.array([x * (0.55 + 0.03 * i)]))[0]
+        step = 2.0 ** (max(np.frexp(low)[1] - 1, -126) - 7)
+        even = round(low / step) % 2 == 0                    # then the middle above goes down, and what is just above it must not
+        t = (low + step / 2) * (1 + (1 if even else -1) * 2.0 ** -27)
+        grad = torch.full((n,), x, dtype=torch.float64, device="cuda").bfloat16()
+        grad[1::2] *= -1
+        assert float(grad[0]) == x
+        before = host(grad)
+        f = t / x
+        assert f < 1
+        out = torch.zeros_like(grad)
+        P.clip_grads([grad], f * ob.total_norm([before]), out=[out])
+        want = before * f
+        assert np.array_equal(nearest_bf16(want), np.sign(before) * (low + step * even))
+        assert np.array_equal(host(out), nearest_bf16(want)), (x, f)
+        wrong += int((host(torch.from_numpy(want).float().bfloat16()) != host(out)).any())
+    assert wrong == 12                                       # (the cases are such)
+
+
 def test_clipping_any_alignment_and_order(P):
     import torch
     g = gen(3)
