@@ -1,8 +1,9 @@
 """What a training step needs around a layer of experts: ctypes binding of the layer norm, the router's balance loss, the norm of all gradients
 and their clipping (same names as the C entry points, argument marshalling only).
 
-As in the layer of experts, gradients are calls of their own, results carry no graph, and nothing here waits for the device.  Matrices may have
-any row stride; their columns are contiguous.
+As in the layer of experts, gradients are calls of their own, results carry no graph, and nothing here waits for the device.  While torch records
+a graph, every call refuses arguments that require a gradient, the gradients' calls among them: second derivatives would be lost.  Matrices may
+have any row stride; their columns are contiguous.
 
 `stream` (None: torch's current stream) is where a call runs.  What it allocates is that stream's memory; as with any work on several streams, the
 caller makes `stream` wait for the arguments, keeps them until it has read them, and waits for it before using the results elsewhere."""
@@ -61,6 +62,8 @@ def layernorm_fwd(x, gamma=None, beta=None, eps=1e-5, out=None, out_dtype=None, 
 def layernorm_bwd(dy, x, mean, rstd, gamma=None, dx=None, dgamma=None, dbeta=None, accumulate=False, weights=True, stream=None):
     """polydl_layernorm_bwd: NormGradients(dx [T][D] of x's type, dgamma [D], dbeta [D] float32).  accumulate adds to the dgamma and dbeta that
     are given; weights=False leaves them out (None)."""
+    if dy.requires_grad or x.requires_grad or mean.requires_grad or rstd.requires_grad or gamma is not None and gamma.requires_grad:
+        _no_graph()
     (T, D), dev = x.shape, _device()
     if not weights and (accumulate or dgamma is not None or dbeta is not None):
         raise ValueError("weights=False forms neither dgamma nor dbeta")
@@ -102,12 +105,14 @@ def balance(logits, ids, stream=None):
 def balance_bwd(logits, counts, rows, dloss=1.0, out=None, accumulate=False, stream=None):
     """polydl_balance_bwd: the gradient of the logits [T][E] from that of the loss, a number or a float32 tensor of one value; accumulate adds it
     to out."""
+    given = isinstance(dloss, torch.Tensor)
+    if logits.requires_grad or given and dloss.requires_grad:
+        _no_graph()
     (T, E), dev = logits.shape, _device()
     if accumulate and out is None:
         raise ValueError("accumulate needs out")
     if out is None:
         out = _new((T, E), torch.float32, logits, stream)
-    given = isinstance(dloss, torch.Tensor)
     for t, name in ((rows, "rows"),) + (((dloss, "dloss"),) if given else ()):
         if t.numel() != 1:
             raise ValueError("%s must hold one value" % name)

@@ -180,3 +180,19 @@ def test_mx4_product_refuses_rows_that_are_not_filled_up():
         for call in (lambda: P.mx4_gemm(x, w), lambda: P.mx4_gemm(x, P.Mx4(w.q[None], w.scales[None]), offsets=torch.zeros(2, dtype=torch.int32))):
             with pytest.raises(ValueError, match="128"):
                 call()
+
+
+def test_second_derivatives_that_would_be_lost_are_refused():
+    # the gradients' own arguments, before anything else is looked at
+    import torch
+    x, w, one = torch.ones(4, 8), torch.ones(8), torch.ones(4)
+    counts, rows = torch.zeros(8, dtype=torch.int32), torch.zeros((), dtype=torch.int32)
+    norm = lambda dy=x, x=x, mean=one, rstd=one, gamma=w: P.layernorm_bwd(dy, x, mean, rstd, gamma)      # noqa: E731
+    balance = lambda logits=x, dloss=torch.ones(1): P.balance_bwd(logits, counts, rows, dloss)           # noqa: E731
+    for f, name, t in [(norm, n, x) for n in ("dy", "x")] + [(norm, n, one) for n in ("mean", "rstd")] + [(norm, "gamma", w), (balance, "logits", x),
+                                                                                                          (balance, "dloss", torch.ones(1))]:
+        leaf = t.clone().requires_grad_()
+        with pytest.raises(RuntimeError, match="requires its gradient"):
+            f(**{name: leaf})
+        with torch.no_grad(), pytest.raises(TypeError, match="memory"):                                  # (the next check, on any machine)
+            f(**{name: leaf})
