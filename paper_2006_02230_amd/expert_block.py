@@ -14,7 +14,8 @@ BlockGradients = collections.namedtuple("BlockGradients", "x gamma beta router w
 
 
 class ExpertBlock:
-    """out = x + layer(layernorm(x)), x [T][D] bfloat16, gamma and beta [D] float32, layer an ExpertLayer.
+    """out = x + layer(layernorm(x)), x [T][D] bfloat16, gamma and beta [D] float32, layer an ExpertLayer.  What the norm and the layer give is bfloat16, as
+    by themselves, and so is their sum with x.
 
     `forward` leaves what `backward` needs in `kept`; with several forwards before their backwards, take it from there after each and give it to its
     backward."""
@@ -43,8 +44,10 @@ class ExpertBlock:
             kept = self.kept
         x, norm, layer = kept
         inner = self.layer.backward(dout, layer)
-        d = Y.layernorm_bwd(inner.x, x, norm.mean, norm.rstd, self.gamma)
-        return BlockGradients(d.dx.add_(dout), d.dgamma, d.dbeta, inner.router, inner.w1, inner.w2)
+        # The norm's gradient in float32, so that its sum with what comes past the layer is rounded once.  A sum of two bfloat16 values has 1.28 times the error
+        # (2.1e-3 of the sum's norm where it is 1.65e-3); the whole backward takes 2404 us with one and 2464 so (8192 rows of 2048, 4 of 16 experts of 4096).
+        d = Y.layernorm_bwd(inner.x, x.float(), norm.mean, norm.rstd, self.gamma)
+        return BlockGradients(torch.add(d.dx, dout, out=torch.empty_like(x)), d.dgamma, d.dbeta, inner.router, inner.w1, inner.w2)
 
     def microscaled(self):
         """The same block with its experts' products in microscaled 4-bit floating point; it answers."""

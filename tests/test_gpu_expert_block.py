@@ -92,6 +92,23 @@ def test_block_gradient_against_differences(L):
     assert abs(slopes[1] - want) <= 4 * noise + 2 * abs(slopes[0] - slopes[1]) + 0.02 * float(grads.gamma.norm() * dg.norm())
 
 
+@pytest.mark.parametrize("T,D", [(1, 64), (40, 72), (700, 256)])
+def test_rows_gradient_is_rounded_once(L, T, D):
+    # the norm's part in float32 and what comes past the layer: their sum, rounded to float32 (2^-24 of it) and to bfloat16 (2^-8)
+    import torch
+    from paper_2006_02230_amd import layernorm_bwd
+    g = gen(T)
+    block = make(L, g, D, 96, 4, 2, 0.5)
+    x, dout = randn(g, T, D).bfloat16(), randn(g, T, D).bfloat16()
+    block.forward(x)
+    _, norm, layer = block.kept
+    inner = block.layer.backward(dout, layer)
+    want = layernorm_bwd(inner.x, x.float(), norm.mean, norm.rstd, block.gamma).dx.double() + dout.double()
+    got = block.backward(dout, block.kept).x
+    assert got.dtype == torch.bfloat16
+    assert bool(((got.double() - want).abs() <= want.abs() * (2.0 ** -8 + 1.01 * 2.0 ** -24)).all())
+
+
 def test_several_forwards_and_a_forward_that_keeps_nothing(L):
     import torch
     g = gen(5)
