@@ -310,6 +310,34 @@ def test_results_do_not_depend_on_the_run_or_the_other_rows(P):
         assert torch.equal(P.mx4_gemm(x, w, offsets=o, out_dtype=torch.float32), first)
 
 
+# by the rule: few rows of one matrix and of several, tiles of 64, of 128 and of 256
+@pytest.mark.parametrize("E,M,N,K", [(1, 16, 70, 900), (3, 20, 300, 520), (2, 700, 500, 900), (1, 2500, 2300, 400), (2, 9000, 3000, 300)])
+@pytest.mark.parametrize("gather", [False, True])
+def test_rows_do_not_depend_on_the_other_rows(P, E, M, N, K, gather):
+    # every third row kept, what is around it in its tile and in the other groups changed: other values, far larger ones, blocks of NaN, zeros, rows that are
+    # none; the kept rows' results are the same bits, and so are the columns' whose neighbours change
+    import torch
+    g = gen(M + N)
+    a, b = randn(g, M, K), randn(g, E, N, K)
+    o = offsets_of(g, E, M)
+    rows = torch.randperm(M, generator=g, device="cuda").int() if gather else None
+    kept = torch.arange(M, device="cuda") % 3 == 1
+    want = P.mx4_gemm(P.mx4_quantise(a), P.mx4_quantise(b), offsets=o, rows=rows, out_dtype=torch.float32)
+    at = kept if rows is None else kept[rows.long()]
+    w = P.mx4_quantise(b)
+    for fill in (None, 1e30, float("nan"), 0.0):
+        other = torch.where(kept[:, None], a, randn(g, M, K) if fill is None else torch.full((), fill, device="cuda"))
+        got = P.mx4_gemm(P.mx4_quantise(other), w, offsets=o, rows=rows, out_dtype=torch.float32)
+        assert torch.equal(got[at], want[at]) and not torch.equal(got, want)
+    if rows is not None:
+        got = P.mx4_gemm(P.mx4_quantise(a), w, offsets=o, rows=torch.where(at, rows, -1).int(), out_dtype=torch.float32)
+        assert torch.equal(got[at], want[at]) and not got[~at].any()
+    column = torch.arange(N, device="cuda") % 5 == 2
+    c = torch.where(column[None, :, None], b, torch.full((), float("nan"), device="cuda"))
+    got = P.mx4_gemm(P.mx4_quantise(a), P.mx4_quantise(c), offsets=o, rows=rows, out_dtype=torch.float32)
+    assert torch.equal(got[:, column], want[:, column]) and bool(torch.isnan(got[:, ~column]).all())
+
+
 def test_captured_and_replayed_and_on_another_stream(P):
     import torch
     g = gen(31)
