@@ -112,67 +112,55 @@ __device__ __forceinline__ mx4_f32x4 mx4_few_mfma(const Mx4Held &a, const Mx4Hel
 #endif
 }
 
-// WAVES waves share a tile of 16 outputs * RT by 16 rows * CT.
-template <int RT, int CT, int WAVES, bool OUT_F32>
+// WAVES waves share a tile of 16 outputs * RT by 16 rows.
+template <int RT, int WAVES, bool OUT_F32>
 __global__ __launch_bounds__(WAVES * 64) void mx4_few_kernel(Mx4Problem p, int col_tiles)
 {
-    __shared__ mx4_f32x4 sums[WAVES][RT * CT][64];
+    __shared__ mx4_f32x4 sums[WAVES][RT][64];
     const int tid = threadIdx.x, lane = tid & 63, wave = wave_value(tid >> 6), col = lane & 15, quad = lane >> 4;
     GroupTile t;
     GroupTiles all;
-    all.init(p.offsets, p.E, p.M, 16 * CT, col_tiles);
+    all.init(p.offsets, p.E, p.M, 16, col_tiles);
     if (!all.find((int)block_number(), &t)) return;
-    const int m0 = t.lo + t.m * 16 * CT, rows = min(16 * CT, t.hi - m0), n0 = t.n * RT * 16;
+    const int m0 = t.lo + t.m * 16, rows = min(16, t.hi - m0), n0 = t.n * RT * 16;
     const int steps = t.e < p.E ? (p.KB + 7) / 8 : 0;                                       // slots behind the last group: zeros
-    const uint8_t *x[CT], *xs[CT], *w[RT], *ws[RT];
-#pragma unroll
-    for (int c = 0; c < CT; ++c) {
-        const int r = c * 16 + col;
-        int src = -1;
-        if (r < rows) {
-            src = p.rows ? p.rows[m0 + r] : m0 + r;
-            if ((unsigned)src >= (unsigned)p.x_rows) src = -1;
-        }
-        x[c] = src < 0 ? nullptr : p.xq + (int64_t)src * p.KB * 16;
-        xs[c] = src < 0 ? nullptr : p.xs + (int64_t)src * p.KB;
+    const uint8_t *w[RT], *ws[RT];
+    int src = -1;
+    if (col < rows) {
+        src = p.rows ? p.rows[m0 + col] : m0 + col;
+        if ((unsigned)src >= (unsigned)p.x_rows) src = -1;
     }
+    const uint8_t *const x = src < 0 ? nullptr : p.xq + (int64_t)src * p.KB * 16, *const xs = src < 0 ? nullptr : p.xs + (int64_t)src * p.KB;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int64_t n = (int64_t)min(t.e, p.E - 1) * p.N + min(n0 + r * 16 + col, p.N - 1);
         w[r] = p.wq + n * p.KB * 16;
         ws[r] = p.ws + n * p.KB;
     }
-    mx4_f32x4 total[RT][CT];
+    mx4_f32x4 total[RT];
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) total[r][c] = mx4_f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int r = 0; r < RT; ++r) total[r] = mx4_f32x4{0.f, 0.f, 0.f, 0.f};
     for (int s = wave; s < steps; s += WAVES) {
-        Mx4Held a[RT], b[CT];
+        Mx4Held a[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) a[r] = mx4_pair(w[r], ws[r], s, quad, p.KB);
+        const Mx4Held b = mx4_pair(x, xs, s, quad, p.KB);
 #pragma unroll
-        for (int c = 0; c < CT; ++c) b[c] = mx4_pair(x[c], xs[c], s, quad, p.KB);
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int c = 0; c < CT; ++c) total[r][c] = mx4_few_mfma<1>(a[r], b[c], mx4_few_mfma<0>(a[r], b[c], total[r][c]));
+        for (int r = 0; r < RT; ++r) total[r] = mx4_few_mfma<1>(a[r], b, mx4_few_mfma<0>(a[r], b, total[r]));
     }
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
-#pragma unroll
-        for (int c = 0; c < CT; ++c) sums[wave][r * CT + c][lane] = total[r][c];
+    for (int r = 0; r < RT; ++r) sums[wave][r][lane] = total[r];
     __syncthreads();
     const bool whole = (p.ldy & 3) == 0 && ((uintptr_t)p.y & 15) == 0;
-    for (int i = wave; i < RT * CT; i += WAVES) {
-        mx4_f32x4 v = sums[0][i][lane];
+    for (int r = wave; r < RT; r += WAVES) {
+        mx4_f32x4 v = sums[0][r][lane];
 #pragma unroll
-        for (int o = 1; o < WAVES; ++o) v += sums[o][i][lane];
-        const int r = i / CT, row = (i - r * CT) * 16 + col, n = n0 + r * 16 + quad * 4, left = p.N - n;
-        if (row >= rows || left <= 0) continue;
+        for (int o = 1; o < WAVES; ++o) v += sums[o][r][lane];
+        const int n = n0 + r * 16 + quad * 4, left = p.N - n;
+        if (col >= rows || left <= 0) continue;
 #pragma unroll
         for (int q = 0; q < 4; ++q) v[q] = mx4_act(v[q], p.act);
-        const int64_t at = (m0 + row) * p.ldy + n;
+        const int64_t at = (m0 + col) * p.ldy + n;
         if constexpr (OUT_F32) {
             float *y = static_cast<float *>(p.y) + at;
             if (whole && left >= 4) {
@@ -195,14 +183,14 @@ __global__ __launch_bounds__(WAVES * 64) void mx4_few_kernel(Mx4Problem p, int c
     }
 }
 
-template <int RT, int CT, int WAVES>
+template <int RT, int WAVES>
 static hipError_t mx4_few_run(const Mx4Problem &p, hipStream_t st)
 {
     const int64_t groups = p.M < p.E + 1 ? p.M : p.E + 1, col_tiles = ((p.N + 15) / 16 + RT - 1) / RT;
-    const int64_t tiles = (p.M + groups * (16 * CT - 1)) / (16 * CT) * col_tiles;
+    const int64_t tiles = (p.M + groups * 15) / 16 * col_tiles;
     if (tiles > kMaxBlocks) return hipErrorInvalidValue;
-    if (p.out_f32) return launch_kernel((mx4_few_kernel<RT, CT, WAVES, true>), many_blocks(tiles, WAVES * 64), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
-    return launch_kernel((mx4_few_kernel<RT, CT, WAVES, false>), many_blocks(tiles, WAVES * 64), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
+    if (p.out_f32) return launch_kernel((mx4_few_kernel<RT, WAVES, true>), many_blocks(tiles, WAVES * 64), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
+    return launch_kernel((mx4_few_kernel<RT, WAVES, false>), many_blocks(tiles, WAVES * 64), dim3(WAVES * 64), 0, st, p, (int)col_tiles);
 }
 
 // ---- tiles ------------------------------------------------------------------------------------------------------
@@ -606,7 +594,7 @@ hipError_t mx4_gemm_launch(const Mx4Problem &p, hipStream_t st)
         // two tiles of outputs share the rows' loads; with fewer workgroups than compute units that costs more than it saves (one row, 4096 x 4096: 5.6
         // us with one tile and eight waves, 6.8 with two; 32 rows of 64 experts, 2048 x 4096: 32 with one, 27 with two and four waves)
         const int64_t chunks = p.M < p.E ? p.M : p.E, tiles = chunks * ((p.N + 31) / 32);
-        return tiles < cus ? mx4_few_run<1, 1, 8>(p, st) : mx4_few_run<2, 1, 4>(p, st);
+        return tiles < cus ? mx4_few_run<1, 8>(p, st) : mx4_few_run<2, 4>(p, st);
     }
     // offsets inside a tile (rows by index: inside the tensor) below 2^32
     if ((p.rows && p.x_rows > 256 ? (int64_t)p.x_rows : 256ll) * p.KB * 16 < 0xf0000000ll) {
