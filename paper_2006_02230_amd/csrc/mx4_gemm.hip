@@ -130,7 +130,11 @@ __global__ __launch_bounds__(WAVES * 64) void mx4_few_kernel(Mx4Problem p, int c
         src = p.rows ? p.rows[m0 + col] : m0 + col;
         if ((unsigned)src >= (unsigned)p.x_rows) src = -1;
     }
-    const uint8_t *const x = src < 0 ? nullptr : p.xq + (int64_t)src * p.KB * 16, *const xs = src < 0 ? nullptr : p.xs + (int64_t)src * p.KB;
+    const uint8_t *x = nullptr, *xs = nullptr;
+    if (src >= 0) {
+        x = p.xq + (int64_t)src * p.KB * 16;
+        xs = p.xs + (int64_t)src * p.KB;
+    }
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int64_t n = (int64_t)min(t.e, p.E - 1) * p.N + min(n0 + r * 16 + col, p.N - 1);
