@@ -36,11 +36,7 @@ class ExpertBlock:
         """BlockGradients(x bfloat16, the others float32) of the forward that left `kept` (None: the only one since the last backward), from the
         gradient of what it gave; the layer's balance loss, times its share, belongs to the loss."""
         if kept is None:
-            if self.kept is None:
-                raise RuntimeError("backward needs a forward that keeps")
-            if self.layer.waiting > 1:
-                raise RuntimeError("%d forwards wait for their backward: give backward the one's `kept`, and keep=False to a forward without "
-                                   "a backward" % self.layer.waiting)
+            self.layer._only(self.kept and self.kept[2])
             kept = self.kept
         x, norm, layer = kept
         inner = self.layer.backward(dout, layer)

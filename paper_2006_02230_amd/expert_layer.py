@@ -33,6 +33,7 @@ class ExpertLayer:
     def __init__(self, router, w1, w2, k, balance=0.0):
         self.router, self.w1, self.w2, self.k, self.balance = router, w1, w2, k, balance
         self.kept, self.waiting, self.used = None, 0, None
+        self.done = False                                   # what `kept` is of has had its backward
 
     def forward(self, x, keep=True):
         """out [T][D] bfloat16.  keep=False: an answer without a backward, of which nothing is kept."""
@@ -43,20 +44,14 @@ class ExpertLayer:
         y = X.grouped_gemm_bf16(h, self.w2, r.offsets)
         if keep:
             self.used = Y.balance(logits, r.ids) if self.balance else None
-            self.kept, self.waiting = (x, xf, logits, r, h, y, self.used), self.waiting + 1
+            self.kept, self.waiting, self.done = (x, xf, logits, r, h, y, self.used), self.waiting + 1, False
         return X.combine_bf16(y, r.slots, r.weights)
 
     def backward(self, dout, kept=None):
         """Gradients(x bfloat16, router, w1, w2 float32) of the forward that left `kept` (None: the only one since the last backward), from the
         gradient of what it gave."""
-        if kept is None:
-            if self.kept is None:
-                raise RuntimeError("backward needs a forward that keeps")
-            if self.waiting > 1:
-                raise RuntimeError("%d forwards wait for their backward: give backward the one's `kept`, and keep=False to a forward without "
-                                   "a backward" % self.waiting)
-            kept = self.kept
-        self.waiting = max(self.waiting - 1, 0)
+        kept = self._only(self.kept) if kept is None else kept
+        self.waiting, self.done = max(self.waiting - 1, 0), self.done or kept is self.kept
         x, xf, logits, r, h, y, used = kept
         dy, dweights = X.combine_bwd_bf16(dout, y, r.slots, r.weights)
         dh = X.grouped_gemm_dx_bf16(dy, self.w2, r.offsets, h=h, act="relu")
@@ -71,6 +66,17 @@ class ExpertLayer:
         drouter = B.sgemm(xf.t().contiguous(), dlogits, torch.empty_like(self.router), alpha=1.0, beta=0.0)
         B.sgemm(dlogits, self.router.t().contiguous(), dx)                     # added to what came through the experts
         return Gradients(dx.bfloat16(), drouter, dw1, dw2)
+
+    def _only(self, kept):
+        """kept, where it was left by the only forward that waits for its backward."""
+        if kept is None:
+            raise RuntimeError("backward needs a forward that keeps")
+        if self.waiting > 1:
+            raise RuntimeError("%d forwards wait for their backward: give backward the one's `kept`, and keep=False to a forward without "
+                               "a backward" % self.waiting)
+        if self.waiting and self.done and kept is self.kept:
+            raise RuntimeError("the last forward has had its backward: give backward the `kept` of the one that waits for its")
+        return kept
 
     def coded(self, group=128, asymmetric=False):
         """The same layer with its experts' weights in 4 bits."""

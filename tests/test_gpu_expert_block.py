@@ -132,6 +132,29 @@ def test_several_forwards_and_a_forward_that_keeps_nothing(L):
         make(L, g, 64, 96, 4, 2, 0.1).backward(dout[0])
 
 
+def test_a_backward_without_kept_is_never_of_another_forward(L):
+    # two forwards, the backward of the last one by its `kept`: the first one still waits, and what the block holds is not its
+    import torch
+    g = gen(8)
+    block = make(L, g, 64, 96, 4, 2, 0.1)
+    layer = block.layer
+    x, y, dout = (randn(g, 30, 64).bfloat16() for _ in range(3))
+    for what, leave in ((block, lambda: block.kept), (layer, lambda: layer.kept)):
+        what.forward(x)
+        first = leave()
+        what.forward(y)
+        want = what.backward(dout, leave())
+        with pytest.raises(RuntimeError, match="has had its backward"):
+            what.backward(dout)
+        other = what.backward(dout, first)
+        # now none waits, and the last forward's may be asked for again
+        for a, b, c in zip(what.backward(dout), want, other):
+            assert torch.equal(a, b) and not torch.equal(a, c)
+        what.forward(x)
+        for a, b in zip(what.backward(dout), other):
+            assert torch.equal(a, b)
+
+
 def test_block_without_tokens(L):
     import torch
     g = gen(6)
