@@ -338,7 +338,8 @@ int polydl_w4_gemm_bf16(int E, int M, int N, int K, int group, const int32_t *of
  * y_tj = (x_tj - mean_t) * rstd_t * gamma_j + beta_j.  x of x_type, y of y_type (polydl_type), gamma and beta D floats or NULL (ones, zeros).
  * mean and rstd (T floats each) are what the gradient needs; each may be NULL.  eps >= 0.  A row of equal values gives y = beta, with eps = 0 an
  * infinite rstd, and NaN where the formula has 0 * infinity.  y is formed from the mean before it is rounded to a float, so a mean of many times the row's
- * spread costs none of its bits.  The squares are summed as floats: where their sum passes the largest one (values from about 2^60 on) rstd is 0.
+ * spread costs none of its bits.  Sums are floats: where that of the squares passes the largest one (values from about 2^57 on) rstd is 0, where that of
+ * the values does y is NaN.
  * polydl_layernorm_bwd: from dy [T][D] (dy_type), with h = (x - mean) * rstd and g = dy * gamma,
  *   dx_tj = rstd_t * (g_tj - sum_i g_ti / D - h_tj * sum_i g_ti h_ti / D), of x_type;
  *   dgamma_j = sum_t dy_tj h_tj, dbeta_j = sum_t dy_tj, float32; accumulate != 0 adds to what they hold.

@@ -592,8 +592,8 @@ static int64_t mx4_rounds(const Mx4Problem &p, int64_t tile, int64_t at_a_time)
 hipError_t mx4_gemm_launch(const Mx4Problem &p, hipStream_t st)
 {
     const int64_t rows = ((int64_t)p.M + p.E - 1) / p.E, cus = compute_units();           // rows of a group, in the mean
-    // One matrix and up to 16 rows (16 rows, 8192 x 8192: 12.7 us, in tiles of 64 16.1), or up to 8 rows a group, where tiles are as fast for many
-    // weights but slower for few (64 groups of 4 rows, 2048 x 4096: 64 / 66 us, 16 of 4 rows, 1024 x 1024: 5.6 / 6.4; but 64 of 16 rows: 97 / 73).
+    // One matrix and up to 16 rows (16 rows, 8192 x 8192: 12.4 us, in tiles of 64 17.4), or up to 8 rows a group, where tiles are as fast for many
+    // weights but slower for few (64 groups of 4 rows, 2048 x 4096: 67 / 64 us, 16 of 4 rows, 1024 x 1024: 4.9 / 5.9; but 64 of 16 rows: 97 / 73).
     if (rows <= (p.E == 1 ? 16 : 8)) {
         // two tiles of outputs share the rows' loads; with fewer workgroups than compute units that costs more than it saves (one row, 4096 x 4096: 5.6
         // us with one tile and eight waves, 6.8 with two; 32 rows of 64 experts, 2048 x 4096: 32 with one, 27 with two and four waves)
@@ -603,8 +603,9 @@ hipError_t mx4_gemm_launch(const Mx4Problem &p, hipStream_t st)
     // offsets inside a tile (rows by index: inside the tensor) below 2^32
     if ((p.rows && p.x_rows > 256 ? (int64_t)p.x_rows : 256ll) * p.KB * 16 < 0xf0000000ll) {
         // Tiles of 256 (one workgroup on a compute unit), of 128 or of 64 (two).  A round of 128 takes 0.62 of a round of 256 and does half the work, one of 64
-        // takes a third for an eighth.  64 / 128 / 256, us: one group of 4096 rows, 4096 x 4096, 84 / 48 / 41; 16 uneven ones of 2048 in the mean, 4096 x 2048,
-        // 400 / 210 / 162; of 256, 2048 x 2048, 27 / 24 / 23; of 128 19 / 16 / 21; of 32 13 / 16 / 21; 7 of 286, 777 x 531, 7 / 9 / 15.
+        // takes a third for an eighth.  64 / 128 / 256, us (three sets of random operands in turn, in a graph): one group of 4096 rows, 4096 x 4096, 85 / 47 / 40; 16
+        // uneven ones of 2048 in the mean, 4096 x 2048, 363 / 214 / 169 (3.2 PFLOP/s); of 256, 2048 x 2048, 28 / 20 / 22; of 128 17 / 14 / 18; of 32 11 / 13 / 17; 7
+        // of 286, 777 x 531, 7.5 / 9.6 / 15.
         const double of256 = (double)mx4_rounds(p, 256, cus), of128 = 0.62 * (double)mx4_rounds(p, 128, 2 * cus), of64 = 0.33 * (double)mx4_rounds(p, 64, 2 * cus);
         if (of256 <= of128 && of256 <= of64) return mx4_tile_pick<256, 256, 128, 64, 2>(p, st);
         return of128 <= of64 ? mx4_tile_pick<128, 128, 64, 64, 2>(p, st) : mx4_tile_pick<64, 64, 32, 32, 4>(p, st);
